@@ -7,4 +7,4 @@ The compute lives in ``libvla.so`` (HIP kernels for gfx950 behind a C ABI);
 loads nothing; the binding loads the library on first use and raises if it
 has not been built.
 """
-__all__ = ["synth", "vla"]
+__all__ = ["synth", "vla", "paged"]

@@ -1,0 +1,84 @@
+// Kernel arguments and launchers of the paged key/value cache.
+#pragma once
+#include "common.h"
+
+// The pool and the batch as the kernels see them (include/vla_paged.h).
+struct PagedKV {
+  const void *k, *v;
+  long page_stride, head_stride, tok_stride;   // elements
+  int n_kv, hd, n_pages, page_shift;           // page_tokens = 1 << page_shift
+};
+struct RaggedBatch {
+  const int32_t *start, *kv_len, *pages;
+  int n_req, n_tok, max_new, max_len, pages_stride;
+};
+
+struct AppendArgs {
+  PagedKV kv;
+  RaggedBatch bt;
+  const void *kin, *vin, *q;
+  void* qo;
+  long k_ts, k_hs, v_ts, v_hs, q_ts, q_hs, qo_ts, qo_hs;
+  int n_q, n_axes, s1, s2;                     // pairs of axis 0 end at s1, of axis 1 at s2
+  int half;                                    // pairs (0: no rotation)
+  const int32_t* pos;
+  double step;                                 // -log2(rope_base) / half
+};
+void launch_append(const AppendArgs& a, int et, hipStream_t s);
+
+struct PagedAttnArgs {
+  PagedKV kv;
+  RaggedBatch bt;
+  const void* q;
+  void* o;
+  long q_ts, q_hs, o_ts, o_hs;
+  float* lse;
+  int n_q, G;                                  // G = n_q / n_kv
+  float scale, cap;
+  int causal, window;
+  const int32_t* prefix;
+  int shared_len;                              // keys below it: pages of request 0
+  float* ws;
+};
+size_t paged_attention_ws(const PagedAttnArgs& a, int et);
+void launch_paged_attention(const PagedAttnArgs& a, int et, hipStream_t s);
+
+// ---------------------------------------------------------------- device side
+struct ReqSpan { int first, n, len; };         // first row, new tokens, tokens in the cache
+
+// Request r's rows and lengths, cut to the stated bounds.
+__device__ __forceinline__ ReqSpan span_of(const RaggedBatch& b, int r, int page_shift) {
+  const int s0 = b.start[r], s1 = b.start[r + 1];
+  ReqSpan p;
+  p.first = s0 < 0 ? 0 : (s0 > b.n_tok ? b.n_tok : s0);
+  const int e = s1 > b.n_tok ? b.n_tok : s1;
+  p.n = e - p.first;
+  if (p.n > b.max_new) p.n = b.max_new;
+  if (p.n < 0) p.n = 0;
+  const long cap = (long)b.pages_stride << page_shift;
+  int len = b.kv_len[r];
+  if (len > b.max_len) len = b.max_len;
+  if (len > cap) len = (int)cap;
+  p.len = len < 0 ? 0 : len;
+  return p;
+}
+
+// The request of a token: the last r with start[r] <= tok (requests without
+// tokens share their start with the next one); n_req when tok lies behind the
+// last. A wavefront looks at 64 starts at a time, so up to 4096 requests take
+// two rounds of loads. Wave-uniform tok; all lanes of the wave call it.
+__device__ __forceinline__ int request_of(const RaggedBatch& b, int tok) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = b.n_req + 1;                 // start[lo] <= tok is known or assumed
+  while (n > 1) {
+    const int step = (n + 63) / 64, i = lo + lane * step;
+    const bool le = i < lo + n && b.start[i] <= tok;
+    const unsigned long long m = __ballot(le);
+    if (m == 0) return b.n_req;                // (starts that do not begin at 0)
+    const int last = 63 - __builtin_clzll(m);
+    const int end = lo + n;
+    lo += last * step;
+    n = end - lo < step ? end - lo : step;
+  }
+  return lo;
+}

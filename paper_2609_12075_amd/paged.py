@@ -1,0 +1,239 @@
+"""Paged key/value cache: ctypes binding of include/vla_paged.h.
+
+Keys and values of a layer live in pages of a pool (``KVPool``); a ``Batch``
+says which tokens each request brings, how long its context then is and on
+which pages it lies. ``append`` writes a step's keys and values (rotating
+queries and keys on the way), ``attention`` attends over the cache and
+``shared_attention`` reads a context that all requests begin with once for
+the batch. Calls run on the pool's device, on `stream` or that device's
+current stream.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Sequence
+
+from . import vla
+
+EXPORTS = ["vla_kv_append", "vla_attention_workspace", "vla_paged_attention", "vla_shared_attention"]
+
+_ci, _vp, _i64 = ctypes.c_int, ctypes.c_void_p, ctypes.c_int64
+
+
+class KVPoolC(ctypes.Structure):
+    _fields_ = [("device", _ci), ("dtype", _ci), ("n_kv", _ci), ("head_dim", _ci), ("page_tokens", _ci),
+                ("n_pages", _ci), ("k", _vp), ("v", _vp), ("page_stride", _i64), ("head_stride", _i64),
+                ("token_stride", _i64)]
+
+
+class RaggedC(ctypes.Structure):
+    _fields_ = [("n_req", _ci), ("n_tok", _ci), ("max_new", _ci), ("max_len", _ci), ("start", _vp), ("kv_len", _vp),
+                ("pages", _vp), ("pages_stride", _ci)]
+
+
+class AppendArgsC(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_tok_stride", _i64), ("k_head_stride", _i64), ("v_tok_stride", _i64),
+                ("v_head_stride", _i64), ("n_q", _ci), ("q", _vp), ("q_out", _vp), ("q_tok_stride", _i64),
+                ("q_head_stride", _i64), ("qo_tok_stride", _i64), ("qo_head_stride", _i64), ("n_axes", _ci),
+                ("sections", _ci * 3), ("positions", _vp), ("rope_base", ctypes.c_float)]
+
+
+class AttentionArgsC(ctypes.Structure):
+    _fields_ = [("q", _vp), ("o", _vp), ("q_tok_stride", _i64), ("q_head_stride", _i64), ("o_tok_stride", _i64),
+                ("o_head_stride", _i64), ("lse", _vp), ("n_q", _ci), ("scale", ctypes.c_float), ("cap", ctypes.c_float),
+                ("causal", _ci), ("window", _ci), ("prefix", _vp), ("ws", _vp), ("ws_bytes", ctypes.c_size_t)]
+
+
+_L = None
+
+
+def _lib():
+    global _L
+    if _L is None:
+        L = vla.lib()
+        P = ctypes.POINTER
+        L.vla_kv_append.argtypes = [P(KVPoolC), P(RaggedC), P(AppendArgsC), _vp]
+        L.vla_attention_workspace.argtypes = [P(KVPoolC), P(RaggedC), P(AttentionArgsC), _ci, P(ctypes.c_size_t)]
+        L.vla_paged_attention.argtypes = [P(KVPoolC), P(RaggedC), P(AttentionArgsC), _vp]
+        L.vla_shared_attention.argtypes = [P(KVPoolC), P(RaggedC), P(AttentionArgsC), _ci, _vp]
+        for n in EXPORTS:
+            getattr(L, n).restype = _ci
+        _L = L
+    return _L
+
+
+def _dtype(t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return 1
+    if t.dtype == torch.float32:
+        return 0
+    raise TypeError(f"float32 or bfloat16 tensors, not {t.dtype}")
+
+
+def _i32(t, name, shape, device):
+    import torch
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be a contiguous int32 tensor {shape} on {device}, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+class KVPool:
+    """One layer's pool: k and v [n_pages][n_kv][page_tokens][head_dim] views
+    of one layout (any strides of the outer three dimensions, so a pool kept
+    token-major or layer-interleaved is passed as a view)."""
+
+    def __init__(self, k, v):
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device:
+            raise ValueError("k and v must be 4-d tensors of one shape, layout, type and device")
+        if k.stride(3) != 1 and k.shape[3] > 1:
+            raise ValueError("head_dim must be contiguous")
+        if not k.is_cuda:
+            raise ValueError("the pool must be on a GPU")
+        self.k, self.v = k, v
+        self.device, self.dtype = k.device, k.dtype
+        n, h, p, d = k.shape
+        self.c = KVPoolC(k.device.index, _dtype(k), h, d, p, n, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
+                         k.stride(2))
+
+
+class Batch:
+    """A ragged batch (vla_ragged): start int32 [n_req + 1], kv_len int32
+    [n_req], pages int32 [n_req][entries], all on the pool's device; n_tok rows
+    of the token buffers; max_new and max_len bound the tokens a request
+    brings and has (the tensors may change within these bounds while captured
+    calls are replayed)."""
+
+    def __init__(self, start, kv_len, pages, n_tok: int, max_new: int, max_len: int):
+        n = kv_len.shape[0]
+        dev = kv_len.device
+        if pages.dim() != 2:
+            raise ValueError("pages must be 2-d")
+        self.start, self.kv_len, self.pages = start, kv_len, pages
+        self.device, self.n_req, self.n_tok = dev, n, n_tok
+        self.c = RaggedC(n, n_tok, max_new, max_len, _i32(start, "start", (n + 1,), dev),
+                         _i32(kv_len, "kv_len", (n,), dev), _i32(pages, "pages", (n, pages.shape[1]), dev),
+                         pages.shape[1])
+
+
+def _rows(t, name, pool: KVPool, batch: Batch, heads: Optional[int]):
+    """Checks a token buffer [n_tok][heads][head_dim] and returns (address, token stride, head stride)."""
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != batch.n_tok or shape[2] != pool.c.head_dim or (heads and shape[1] != heads):
+        raise ValueError(f"{name} must be [{batch.n_tok}, {heads or 'heads'}, {pool.c.head_dim}], not {tuple(shape)}")
+    if t.dtype != pool.dtype or t.device != pool.device:
+        raise ValueError(f"{name} must be {pool.dtype} on {pool.device}, not {t.dtype} on {t.device}")
+    ts, hs, ds = t.stride()
+    if ds != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.data_ptr(), ts, hs
+
+
+def _same_device(pool: KVPool, batch: Batch):
+    if batch.device != pool.device:
+        raise ValueError(f"the batch is on {batch.device}, the pool on {pool.device}")
+
+
+def _stream(pool: KVPool, stream):
+    if stream is None:
+        import torch
+        return torch.cuda.current_stream(pool.device).cuda_stream
+    return vla._stream(stream)
+
+
+def append(pool: KVPool, batch: Batch, k, v, q=None, q_out=None, positions=None, sections: Sequence[int] = (),
+           rope_base: float = 10000.0, stream=None):
+    """vla_kv_append. k, v [n_tok][n_kv][head_dim], q [n_tok][n_q][head_dim]
+    (views with contiguous rows); sections: the pairs that each axis turns
+    (empty: no rotation); positions int32 [n_tok][len(sections)] or None (one
+    axis: the tokens' places). Returns q_out (allocated unless given)."""
+    _same_device(pool, batch)
+    n_kv = pool.c.n_kv
+    a = AppendArgsC()
+    a.k, a.k_tok_stride, a.k_head_stride = _rows(k, "k", pool, batch, n_kv)
+    a.v, a.v_tok_stride, a.v_head_stride = _rows(v, "v", pool, batch, n_kv)
+    if q is not None:
+        a.n_q = q.shape[1] if q.dim() == 3 else 0
+        a.q, a.q_tok_stride, a.q_head_stride = _rows(q, "q", pool, batch, None)
+        if q_out is None:
+            import torch
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        a.q_out, a.qo_tok_stride, a.qo_head_stride = _rows(q_out, "q_out", pool, batch, a.n_q)
+    if len(sections) > 3:
+        raise ValueError("at most three axes")
+    a.n_axes = len(sections)
+    for i, s in enumerate(sections):
+        a.sections[i] = s
+    if positions is not None:
+        a.positions = _i32(positions, "positions", (batch.n_tok, len(sections)), pool.device)
+    a.rope_base = rope_base
+    vla._check(_lib().vla_kv_append(ctypes.byref(pool.c), ctypes.byref(batch.c), ctypes.byref(a), _stream(pool, stream)))
+    return q_out
+
+
+def _attend(pool, batch, q, shared_len, out, lse, scale, cap, causal, window, prefix, ws, stream):
+    import torch
+    _same_device(pool, batch)
+    L = _lib()
+    a = AttentionArgsC()
+    a.q, a.q_tok_stride, a.q_head_stride = _rows(q, "q", pool, batch, None)
+    a.n_q = q.shape[1]
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    a.o, a.o_tok_stride, a.o_head_stride = _rows(out, "out", pool, batch, a.n_q)
+    if lse is not None:
+        if lse.dtype != torch.float32 or tuple(lse.shape) != (batch.n_tok, a.n_q) or not lse.is_contiguous() \
+                or lse.device != pool.device:
+            raise ValueError(f"lse must be a contiguous float32 tensor [{batch.n_tok}, {a.n_q}] on {pool.device}")
+        a.lse = lse.data_ptr()
+    a.scale, a.cap, a.causal, a.window = scale, cap, int(bool(causal)), window
+    if prefix is not None:
+        a.prefix = _i32(prefix, "prefix", (batch.n_req,), pool.device)
+    p, b, r = ctypes.byref(pool.c), ctypes.byref(batch.c), ctypes.byref(a)
+    if ws is None:
+        need = ctypes.c_size_t()
+        vla._check(L.vla_attention_workspace(p, b, r, shared_len or 0, ctypes.byref(need)))
+        if need.value:
+            # the allocator hands it out again only behind the calls of the stream it was allocated on
+            ws = torch.empty(need.value, dtype=torch.uint8, device=pool.device)
+            if stream is not None:
+                ws.record_stream(stream if hasattr(stream, "cuda_stream") else
+                                 torch.cuda.ExternalStream(int(stream), device=pool.device))
+    if ws is not None:
+        if ws.device != pool.device or not ws.is_contiguous():
+            raise ValueError(f"ws must be a contiguous tensor on {pool.device}")
+        a.ws, a.ws_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
+    s = _stream(pool, stream)
+    if shared_len is None:
+        vla._check(L.vla_paged_attention(p, b, r, s))
+    else:
+        vla._check(L.vla_shared_attention(p, b, r, shared_len, s))
+    return out
+
+
+def attention(pool: KVPool, batch: Batch, q, out=None, lse=None, scale: float = 0.0, cap: float = 0.0,
+              causal: bool = True, window: int = 0, prefix=None, ws=None, stream=None):
+    """vla_paged_attention. q [n_tok][n_q][head_dim] (a view with contiguous
+    rows); lse float32 [n_tok][n_q] or None; prefix int32 [n_req] or None; ws:
+    a tensor of workspace_bytes(...) bytes or None (allocated for the call).
+    Returns out (allocated unless given; rows behind the last request are not
+    written)."""
+    return _attend(pool, batch, q, None, out, lse, scale, cap, causal, window, prefix, ws, stream)
+
+
+def shared_attention(pool: KVPool, batch: Batch, q, shared_len: int, out=None, lse=None, scale: float = 0.0,
+                     cap: float = 0.0, causal: bool = True, window: int = 0, prefix=None, ws=None, stream=None):
+    """vla_shared_attention: as attention, for a batch whose requests have
+    their first shared_len tokens (whole pages) on the same pages."""
+    return _attend(pool, batch, q, int(shared_len), out, lse, scale, cap, causal, window, prefix, ws, stream)
+
+
+def workspace_bytes(pool: KVPool, batch: Batch, n_q: int, shared_len: int = 0, causal: bool = True,
+                    window: int = 0) -> int:
+    """vla_attention_workspace: scratch bytes of such an attention (host only)."""
+    a = AttentionArgsC(n_q=n_q, causal=int(bool(causal)), window=window)
+    need = ctypes.c_size_t()
+    vla._check(_lib().vla_attention_workspace(ctypes.byref(pool.c), ctypes.byref(batch.c), ctypes.byref(a), shared_len,
+                                              ctypes.byref(need)))
+    return need.value
