@@ -96,86 +96,10 @@ __global__ void __launch_bounds__(256) append_kernel(AppendArgs a) {
   }
 }
 
-// ---------------------------------------------------------------- attention
-// One wavefront per (token, query head). A lane scores one of 64 keys, the
-// running maximum and sum of the softmax are the wave's, and then the lanes
-// own four dims each of the output while the keys' values pass.
-template <typename T>
-__global__ void __launch_bounds__(256) paged_row_kernel(PagedAttnArgs a) {
-  __shared__ float qs[4][256];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hd = a.kv.hd;
-  const int tok = blockIdx.x, h = blockIdx.y * 4 + wave;
-  const int r = request_of(a.bt, tok);
-  if (r >= a.bt.n_req || h >= a.n_q) return;
-  const ReqSpan sp = span_of(a.bt, r, a.kv.page_shift);
-  if (tok - sp.first >= sp.n) return;
-  const int p = sp.len - sp.n + tok - sp.first, prefix = a.prefix ? a.prefix[r] : 0, g = h / a.G;
-  const T* q = reinterpret_cast<const T*>(a.q) + (long)tok * a.q_ts + (long)h * a.q_hs;
-  for (int d = lane; d < hd; d += 64) qs[wave][d] = (float)q[d];
-  __builtin_amdgcn_wave_barrier();
-  float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = 0; k0 < sp.len; k0 += 64) {
-    const int j = k0 + lane;
-    const bool vis = j < sp.len && (!a.causal || j < prefix || (j <= p && (!a.window || p - j < a.window)));
-    int page = -1;
-    if (vis) page = a.bt.pages[(j < a.shared_len ? 0L : (long)r * a.bt.pages_stride) + (j >> a.kv.page_shift)];
-    const bool ok = vis && (unsigned)page < (unsigned)a.kv.n_pages;
-    const long off = ok ? (long)page * a.kv.page_stride + (long)g * a.kv.head_stride +
-                              (long)(j & ((1 << a.kv.page_shift) - 1)) * a.kv.tok_stride : 0;
-    float s = -INFINITY;
-    if (ok) {
-      s = 0.f;
-      for (int d = 0; d < hd; d += 8) {
-        float x[8];
-        load8<T>(a.kv.k, off + d, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s = fmaf(x[e], qs[wave][d + e], s);
-      }
-      s *= a.scale;
-      if (a.cap > 0.f) s = a.cap * tanhf(s / a.cap);
-    }
-    float mx = s;
-    for (int w = 32; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor(mx, w));
-    const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn;
-    const float alpha = expf(m - ref), pj = ok ? expf(s - ref) : 0.f;
-    float ps = pj;
-    for (int w = 32; w > 0; w >>= 1) ps += __shfl_xor(ps, w);
-    l = l * alpha + ps;
-    m = mn;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] *= alpha;
-    unsigned long long live = __ballot(ok);
-    while (live) {
-      const int t = __builtin_ctzll(live);
-      live &= live - 1;
-      const float pt = __shfl(pj, t);
-      const long ot = __shfl(off, t);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e * 64 + lane < hd) o[e] = fmaf(pt, (float)reinterpret_cast<const T*>(a.kv.v)[ot + e * 64 + lane], o[e]);
-    }
-  }
-  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // (a NaN sum stays)
-  T* op = reinterpret_cast<T*>(a.o) + (long)tok * a.o_ts + (long)h * a.o_hs;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (e * 64 + lane < hd) op[e * 64 + lane] = (T)(o[e] * inv);
-  if (a.lse && lane == 0) a.lse[(long)tok * a.n_q + h] = m + logf(l);
-}
-
 }  // namespace
 
 void launch_append(const AppendArgs& a, int et, hipStream_t s) {
   if (a.bt.n_tok <= 0) return;
   if (et == ET_BF16) hipLaunchKernelGGL(append_kernel<bf16>, dim3(a.bt.n_tok), dim3(256), 0, s, a);
   else hipLaunchKernelGGL(append_kernel<float>, dim3(a.bt.n_tok), dim3(256), 0, s, a);
-}
-
-size_t paged_attention_ws(const PagedAttnArgs& a, int et) { return 0; }
-
-void launch_paged_attention(const PagedAttnArgs& a, int et, hipStream_t s) {
-  if (a.bt.n_tok <= 0) return;
-  const dim3 grid(a.bt.n_tok, (a.n_q + 3) / 4);
-  if (et == ET_BF16) hipLaunchKernelGGL(paged_row_kernel<bf16>, grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(paged_row_kernel<float>, grid, dim3(256), 0, s, a);
 }

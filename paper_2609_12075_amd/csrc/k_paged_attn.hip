@@ -1,0 +1,1045 @@
+// Attention over a paged key/value cache on gfx950.
+//
+// Rows are (token, query head of a KV head's group) pairs in token-major
+// order, so the query heads that share a KV head read its keys once and a tile
+// of rows spans few places. Both products run on the matrix cores (bf16:
+// v_mfma_f32_32x32x16, 32 rows a wave). The scores are computed transposed
+// (S^T = K Q^T): a lane holds keys of one row only, so the row statistics need
+// one exchange between the lane halves, and the probabilities are the second
+// product's operand as they are (its key order inside 16 keys permuted alike
+// on the V side). Softmax is online in fp32, in log2 units.
+//
+// A key range of a row tile is a list of key tiles: those below the prefix,
+// then those of the window and the causal part; tiles that no row of a block
+// sees are not in it. Only tiles at a border of some row's keys are masked
+// element by element. Ranges of one tile of rows go to different blocks where
+// the rows alone would not fill the chip, and are merged by a second kernel.
+#include <algorithm>
+
+#include "paged.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
+
+// 16 zero bytes: what 16-byte pieces behind the last key or head_dim read
+static __device__ __align__(16) unsigned char zero_piece[16];
+
+// ---------------------------------------------------------------- rows and their keys
+// Row r of a tile sees key j (of the launch's [klo, khi)) when j < pre or lo <= j < hi.
+struct Limits { int pre, lo, hi; };
+
+// What a block computes: rows row0 .. of the nrows rows of request r (or of the
+// batch), the list of key tiles [ubeg, uend) of them, and where results go.
+struct Item {
+  int g, r, row0, nrows, first, place0, len, prefix;
+  int klim;                                    // keys from here on are not read
+  int n1, t2, ntiles;                          // tile list: 0 .. n1 - 1, then t2 ..
+  int ubeg, uend, slot, nranges;
+  const int32_t* pages;
+};
+
+__device__ __forceinline__ Limits limits(const PagedAttnArgs& a, int p, int len, int prefix) {
+  Limits m;
+  if (!a.causal) {
+    m.pre = min(len, a.khi);
+    m.lo = m.hi = 0;
+    return m;
+  }
+  m.pre = min(min(prefix, len), a.khi);
+  m.lo = max(a.klo, a.window ? p - a.window + 1 : 0);
+  m.hi = min(min(p + 1, len), a.khi);
+  return m;
+}
+
+// false: nothing to do. KT keys a tile; lists of keys below the prefix are
+// padded to PAD tiles, so that PAD neighbours of a list are neighbours in the cache.
+template <int BR, int KT, int PAD>
+__device__ __forceinline__ bool find_item(const PagedAttnArgs& a, Item& it) {
+  const RaggedBatch& bt = a.bt;
+  const int L = blockIdx.x, v = L / a.kv.n_kv;
+  it.g = L - v * a.kv.n_kv;                    // KV heads fastest: with eight of them, one on each die
+  // causal row tiles get longer: the long ones first
+  const int tile = a.causal && !a.flat ? a.tiles - 1 - v : v;
+  const int range = blockIdx.y;
+  it.slot = a.slot0 + range;
+  if (a.flat) {
+    const int s0 = max(0, bt.start[0]), s1 = min(bt.n_tok, bt.start[bt.n_req]);
+    it.r = 0;
+    it.first = s0;
+    it.nrows = (s1 - s0) * a.G;
+    it.row0 = tile * BR;
+    it.len = it.klim = a.khi;
+    it.place0 = it.prefix = 0;
+    it.pages = bt.pages;
+    if (it.row0 >= it.nrows) return false;
+    it.n1 = it.ntiles = (a.khi - a.klo + KT - 1) / KT;
+    it.t2 = it.n1;
+  } else {
+    int t = 0;
+    if (bt.max_new * a.G <= BR) {
+      it.r = tile;
+    } else {
+      // request r's tiles begin at start[r] G / BR + r, which leaves room for all of them; the last that begins
+      // at or before `tile`
+      const int lane = threadIdx.x & 63;
+      int lo = 0, n = bt.n_req;
+      while (n > 1) {
+        const int step = (n + 63) / 64, i = lo + lane * step;
+        const bool le = i < lo + n && (int)((long)bt.start[i] * a.G / BR) + i <= tile;
+        const unsigned long long m = __ballot(le);
+        if (m == 0) break;
+        const int last = 63 - __builtin_clzll(m), end = lo + n;
+        lo += last * step;
+        n = min(step, end - lo);
+      }
+      it.r = __builtin_amdgcn_readfirstlane(lo);
+      t = tile - ((int)((long)bt.start[it.r] * a.G / BR) + it.r);
+    }
+    it.prefix = a.prefix ? a.prefix[it.r] : 0;
+    const ReqSpan sp = span_of(bt, it.r, a.kv.page_shift);
+    it.first = sp.first;
+    it.nrows = sp.n * a.G;
+    it.row0 = t * BR;
+    if (t < 0 || it.row0 >= it.nrows) return false;
+    it.len = sp.len;
+    it.place0 = sp.len - sp.n;
+    it.klim = min(sp.len, a.khi);
+    it.pages = bt.pages + (long)it.r * bt.pages_stride;
+    const int last = min(it.row0 + BR, it.nrows) - 1;
+    const Limits m0 = limits(a, it.place0 + it.row0 / a.G, it.len, it.prefix);
+    const Limits m1 = limits(a, it.place0 + last / a.G, it.len, it.prefix);
+    it.n1 = m0.pre > a.klo ? ((m0.pre - a.klo + KT - 1) / KT + PAD - 1) / PAD * PAD : 0;
+    it.t2 = max(it.n1, (m0.lo - a.klo) / KT);
+    const int t2e = m1.hi > a.klo ? (m1.hi - a.klo + KT - 1) / KT : 0;
+    it.ntiles = it.n1 + max(0, t2e - it.t2);
+  }
+  it.nranges = (it.ntiles + a.chunk - 1) / a.chunk;
+  it.ubeg = range * a.chunk;
+  it.uend = min(it.ntiles, it.ubeg + a.chunk);
+  return true;
+}
+
+struct Row { int tok, head; Limits lim; };
+
+// Row `row` of the item (rows behind the last one stand for the last one).
+__device__ __forceinline__ Row row_of(const PagedAttnArgs& a, const Item& it, int row) {
+  Row w;
+  const int rc = min(row, it.nrows - 1), t = rc / a.G;
+  w.tok = it.first + t;
+  w.head = it.g * a.G + rc - t * a.G;
+  if (a.flat) {
+    const int r = lane_request_of(a.bt, w.tok);
+    const ReqSpan sp = span_of(a.bt, r, a.kv.page_shift);
+    w.lim = limits(a, sp.len - sp.n + w.tok - sp.first, sp.len, a.prefix ? a.prefix[r] : 0);
+  } else {
+    w.lim = limits(a, it.place0 + t, it.len, it.prefix);
+  }
+  return w;
+}
+
+__device__ __forceinline__ bool sees(const Limits& m, int j) {
+  return (j < m.pre) | ((unsigned)(j - m.lo) < (unsigned)max(0, m.hi - m.lo));
+}
+
+// The least and largest limits of a wave's rows, for the test of whole tiles.
+struct WaveLimits { int pre0, pre1, lo0, lo1, hi0, hi1; };
+
+template <int ROWS>
+__device__ __forceinline__ WaveLimits wave_limits(const PagedAttnArgs& a, const Limits& m) {
+  WaveLimits w;
+  if (a.flat) {
+    w = {m.pre, m.pre, m.lo, m.lo, m.hi, m.hi};
+#pragma unroll
+    for (int o = ROWS / 2; o > 0; o >>= 1) {
+      w.pre0 = min(w.pre0, __shfl_xor(w.pre0, o)); w.pre1 = max(w.pre1, __shfl_xor(w.pre1, o));
+      w.lo0 = min(w.lo0, __shfl_xor(w.lo0, o)); w.lo1 = max(w.lo1, __shfl_xor(w.lo1, o));
+      w.hi0 = min(w.hi0, __shfl_xor(w.hi0, o)); w.hi1 = max(w.hi1, __shfl_xor(w.hi1, o));
+    }
+    w = {__builtin_amdgcn_readfirstlane(w.pre0), __builtin_amdgcn_readfirstlane(w.pre1),
+         __builtin_amdgcn_readfirstlane(w.lo0), __builtin_amdgcn_readfirstlane(w.lo1),
+         __builtin_amdgcn_readfirstlane(w.hi0), __builtin_amdgcn_readfirstlane(w.hi1)};
+  } else {                                     // limits ascend with the row
+    w.pre0 = w.pre1 = __builtin_amdgcn_readfirstlane(m.pre);
+    w.lo0 = __builtin_amdgcn_readfirstlane(m.lo);
+    w.hi0 = __builtin_amdgcn_readfirstlane(m.hi);
+    w.lo1 = __builtin_amdgcn_readlane(m.lo, ROWS - 1);
+    w.hi1 = __builtin_amdgcn_readlane(m.hi, ROWS - 1);
+  }
+  return w;
+}
+__device__ __forceinline__ bool tile_full(const WaveLimits& w, int k0, int k1) {
+  return k1 <= w.pre0 || (k0 >= w.lo1 && k1 <= w.hi0);
+}
+__device__ __forceinline__ bool tile_unseen(const WaveLimits& w, int k0, int k1) {
+  return k0 >= w.pre1 && (k0 >= w.hi1 || k1 <= w.lo0);
+}
+
+// ---------------------------------------------------------------- small pieces
+// The maximum that passes a NaN on, in one instruction.
+__device__ __forceinline__ float vmax(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float other_half(float v, float& mine) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  mine = __uint_as_float(r[0]);
+  return __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float max_x32(float v) { float m; const float o = other_half(v, m); return vmax(m, o); }
+__device__ __forceinline__ float sum_x32(float v) { float m; const float o = other_half(v, m); return m + o; }
+
+// The capped score in log2 units: cap tanh(s scale / cap) log2 e, with
+// tanh(x) = 1 - 2 / (1 + e^2x); c1 = 2 scale log2 e / cap, c2 = cap log2 e.
+// (hardware exp2 and reciprocal: off by a few 2^-24 of the cap)
+__device__ __forceinline__ float capped(float s, float c1, float c2) {
+  return c2 - 2.f * c2 * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * c1));
+}
+
+// The element offset of a page for this KV head, or -1 where it is not there.
+__device__ __forceinline__ long page_offset(const PagedAttnArgs& a, int id, int g) {
+  return (unsigned)id < (unsigned)a.kv.n_pages ? (long)id * a.kv.page_stride + (long)g * a.kv.head_stride : -1;
+}
+
+__device__ __forceinline__ void store_stats(const PagedAttnArgs& a, long row, int slot, float m, float l) {
+  float* st = a.ws + (long)a.bt.n_tok * a.n_q * a.slots * a.kv.hd + (row * a.slots + slot) * 2;
+  st[0] = m;
+  st[1] = l;
+}
+__device__ __forceinline__ float* part_of(const PagedAttnArgs& a, long row, int slot) {
+  return a.ws + (row * a.slots + slot) * a.kv.hd;
+}
+
+// A range without keys: its statistics say so. (Whole blocks; rows split over the block's threads.)
+template <int BR>
+__device__ __forceinline__ void empty_range(const PagedAttnArgs& a, const Item& it) {
+  for (int i = threadIdx.x; i < BR; i += blockDim.x) {
+    const int row = it.row0 + i;
+    if (row >= it.nrows) break;
+    const int t = row / a.G;
+    store_stats(a, (long)(it.first + t) * a.n_q + it.g * a.G + row - t * a.G, it.slot, -INFINITY, 0.f);
+  }
+}
+
+// ---------------------------------------------------------------- bf16 tiles in LDS
+// Tiles of K and V are key-major rows of HDP elements; the 16-byte piece c of
+// row r sits in slot c ^ swz(r), which keeps the reads of one piece of many
+// rows off each other's banks. They move global -> LDS with the direct loads
+// (lane l's 16 bytes at LDS base + 16 l).
+template <int HDP>
+struct Lay {
+  static constexpr int CR = HDP / 8, ROWB = HDP * 2, RP = CR >= 16 ? 1 : 16 / CR, SWM = (CR >= 16 ? 16 : CR) - 1;
+  static constexpr int HX = CR >= 16 ? 2 : 1;  // eight rows further the swizzle differs by 4 HX pieces
+  __device__ static constexpr int swz(int r) { return (r / RP) & SWM; }
+};
+
+__device__ __forceinline__ unsigned lds_addr(const void* p) {
+  return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char*)(p);
+}
+
+// 16 bytes a lane, global -> LDS (wave-uniform dst + 16 lane). Written out: the
+// compiler, which cannot tell the slots of a ring apart, waits for all of its
+// own direct loads before each LDS read; these loads' waits are in the loops.
+__device__ __forceinline__ void dma16(const void* src, unsigned dst) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(dst) : "memory", "m0");
+}
+
+// V^T fragments of a 16-key group: subtile u (32 dims) holds, of lane l, dim
+// l % 32 of keys 4 (l / 32) + 0..3 and + 8..11: two transposing reads of four
+// keys each. ad[u]: the lane's byte address of subtile u's first read (of
+// subtiles 0 .. 3; 4 .. 7 lie 256 bytes on); off: bytes to the group.
+typedef short v4s __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ bf16x4 read_tr(unsigned at) {
+  typedef __attribute__((address_space(3))) v4s* P;
+  return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)at));
+}
+template <int HDP>
+__device__ __forceinline__ bf16x8 read_vt(const unsigned (&ad)[4], int u, int off) {
+  const bf16x4 l = read_tr(ad[u % 4] + off + u / 4 * 256),
+               h = read_tr(ad[(u % 4) ^ Lay<HDP>::HX] + off + u / 4 * 256 + 8 * Lay<HDP>::ROWB);
+  return __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// The window of page offsets a block keeps in LDS (bytes from the pool's bases
+// of this KV head's rows; -1: not there), entries w0 .. w0 + PW - 1.
+constexpr int PW = 512;
+
+// ---------------------------------------------------------------- bf16, common
+// State of a wave: 32 rows, all dims.
+template <int HDP>
+struct Acc {
+  f32x16 o[HDP / 32];
+  float m, l;                                  // m: reference of the exponents (log2); l: this lane's keys
+};
+
+// One tile of 16 N keys' scores into weights: cap, mask, running maximum, sum.
+// sc[st][i] is key 32 st + 8 (i / 4) + 4 (lane / 32) + i % 4 of the tile.
+template <int HDP, int NS, bool CAP>
+__device__ __forceinline__ void softmax_tile(Acc<HDP>& s, f32x16 (&sc)[NS], float sl2, float c1, float c2, bool full,
+                                             const Limits& lim, int k0, const PagedAttnArgs& a, const Item& it,
+                                             bool holes) {
+  const int h4 = (threadIdx.x & 32) >> 3;
+  if constexpr (CAP) {
+#pragma unroll
+    for (int st = 0; st < NS; ++st)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[st][i] = capped(sc[st][i], c1, c2);
+  }
+  if (!full) {
+#pragma unroll
+    for (int st = 0; st < NS; ++st)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!sees(lim, k0 + st * 32 + (i / 4) * 8 + h4 + i % 4)) sc[st][i] = -INFINITY;
+    if (holes) {
+      unsigned gone = 0;
+#pragma unroll 1
+      for (int i = 0; i < 16 * NS; ++i) {
+        const int j = min(k0 + (i / 4) * 8 + h4 + i % 4, it.klim - 1);
+        gone |= (unsigned)((unsigned)it.pages[j >> a.kv.page_shift] >= (unsigned)a.kv.n_pages) << i;
+      }
+#pragma unroll
+      for (int i = 0; i < 16 * NS; ++i)
+        if (gone >> i & 1) sc[i / 16][i % 16] = -INFINITY;
+    }
+  }
+  float mx = sc[0][0];
+#pragma unroll
+  for (int i = 1; i < 16 * NS; ++i) mx = vmax(mx, sc[i / 16][i % 16]);
+  mx = max_x32(mx);
+  if constexpr (!CAP) mx *= sl2;
+  // (rows that have seen nothing keep a reference of 0: no -inf - -inf)
+  const float mn = vmax(s.m, mx), ref = mn == -INFINITY ? 0.f : mn;
+  const float alpha = __builtin_amdgcn_exp2f(s.m - ref);
+  s.m = mn;
+  float ps[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int st = 0; st < NS; ++st)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float x = CAP ? sc[st][i] - ref : __builtin_fmaf(sc[st][i], sl2, -ref);
+      const float p = __builtin_amdgcn_exp2f(x);
+      sc[st][i] = p;
+      ps[i % 4] += p;
+    }
+  // (the sum takes the weights before their rounding to bf16: one rounding less)
+  s.l = s.l * alpha + ((ps[0] + ps[1]) + (ps[2] + ps[3]));
+#pragma unroll
+  for (int u = 0; u < HDP / 32; ++u) s.o[u] *= alpha;
+}
+
+__device__ __forceinline__ bf16x8 weights_of(const f32x16& s, int c) {
+  bf16x8 p;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) p[e] = (bf16)s[8 * c + e];
+  return p;
+}
+
+// A wave whose outputs are not all finite adds its rows again key by key: a
+// weight of zero times an infinite (or NaN) value that the row does not see is
+// a NaN in the products above. `tile(n)`: first key of the wave's n-th tile.
+template <int HDP, bool CAP, typename Tile>
+__device__ __forceinline__ void repair(const PagedAttnArgs& a, const Item& it, Acc<HDP>& s, const bf16x8 (&qf)[HDP / 16],
+                                       const Limits& lim, float sl2, float c1, float c2, int ntiles, int kt, Tile tile) {
+  float z = 0.f;
+#pragma unroll
+  for (int u = 0; u < HDP / 32; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z = __builtin_fmaf(s.o[u][i], 0.f, z);
+  if (__ballot(z != z) == 0) return;
+  const int h = (threadIdx.x & 32) >> 5, hd = a.kv.hd;
+  const float ref = s.m == -INFINITY ? 0.f : s.m;
+#pragma unroll
+  for (int u = 0; u < HDP / 32; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s.o[u][i] = 0.f;
+#pragma unroll 1
+  for (int n = 0; n < ntiles; ++n) {
+    const int k0 = tile(n);
+#pragma unroll 1
+    for (int j = k0; j < min(k0 + kt, it.klim); ++j) {
+      const bool vis = sees(lim, j);
+      if (__ballot(vis) == 0) continue;
+      const long off = page_offset(a, it.pages[j >> a.kv.page_shift], it.g);
+      if (off < 0) continue;
+      const long at = off + (long)(j & ((1 << a.kv.page_shift) - 1)) * a.kv.tok_stride;
+      const bf16 *kp = reinterpret_cast<const bf16*>(a.kv.k) + at, *vp = reinterpret_cast<const bf16*>(a.kv.v) + at;
+      float d = 0.f;
+#pragma unroll
+      for (int c = 0; c < HDP / 16; ++c)
+        if (16 * c + 8 * h < hd) {
+          const bf16x8 x = *reinterpret_cast<const bf16x8*>(kp + 16 * c + 8 * h);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) d = __builtin_fmaf((float)x[e], (float)qf[c][e], d);
+        }
+      d = sum_x32(d);
+      const float p = __builtin_amdgcn_exp2f((CAP ? capped(d, c1, c2) : d * sl2) - ref);
+#pragma unroll
+      for (int u = 0; u < HDP / 32; ++u)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int dim = 32 * u + 8 * q + 4 * h;
+          if (dim < hd && vis) {
+            const bf16x4 x = *reinterpret_cast<const bf16x4*>(vp + dim);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s.o[u][4 * q + e] = __builtin_fmaf(p, (float)x[e], s.o[u][4 * q + e]);
+          }
+        }
+    }
+  }
+}
+
+// The queries are in registers from here on (else the compiler, which does not
+// know the waits of the loop, waits for all loads before each use of them).
+template <int N>
+__device__ __forceinline__ void hold(bf16x8 (&q)[N]) {
+#pragma unroll
+  for (int c = 0; c < N; ++c) asm volatile("" : "+v"(q[c]));
+}
+
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
+// Four dims of a row: to the output, or to the range's slot.
+__device__ __forceinline__ void put(const PagedAttnArgs& a, const Item& it, const Row& w, bool direct, int dim, f32x4 v,
+                                    float inv) {
+  if (dim >= a.kv.hd) return;
+  if (direct) {
+    bf16* op = reinterpret_cast<bf16*>(a.o) + (long)w.tok * a.o_ts + (long)w.head * a.o_hs + dim;
+    *reinterpret_cast<bf16x4*>(op) = bf16x4{(bf16)(v[0] * inv), (bf16)(v[1] * inv), (bf16)(v[2] * inv), (bf16)(v[3] * inv)};
+  } else {
+    *reinterpret_cast<f32x4*>(part_of(a, (long)w.tok * a.n_q + w.head, it.slot) + dim) = v;
+  }
+}
+// The statistics of a row (one lane of it calls this). direct: the row's log-sum-exp.
+__device__ __forceinline__ void put_stats(const PagedAttnArgs& a, const Item& it, const Row& w, bool direct, float m, float l) {
+  const long row = (long)w.tok * a.n_q + w.head;
+  if (!direct) {
+    store_stats(a, row, it.slot, m, l);
+    return;
+  }
+  if (a.lse) a.lse[row] = (m + __builtin_amdgcn_logf(l)) * LN2;
+  if (a.slots > 1) store_stats(a, row, 0, 0.f, -1.f);
+}
+
+// The lane's byte addresses for read_vt within a tile at LDS address `base`.
+template <int HDP>
+__device__ __forceinline__ void vt_addresses(unsigned base, unsigned (&ad)[4]) {
+  const int lane = threadIdx.x & 63, s = lane & 15, r = 4 * (lane >> 5) + (s >> 2);
+  const int c = 2 * ((lane >> 4) & 1) + ((s & 3) >> 1);
+  const unsigned a0 = r * Lay<HDP>::ROWB + ((c ^ Lay<HDP>::swz(r)) << 4) + ((s & 1) << 3);
+#pragma unroll
+  for (int u = 0; u < 4; ++u) ad[u] = base + (a0 ^ (u << 6));
+}
+
+// Fills the window of page offsets from entry e0 on; true where a page that
+// the item's keys need is not there.
+// (256 threads, all of them call it, and none reads the window or the flags
+// of an earlier call any more; ends with a barrier)
+struct Window { long off[PW]; int flag[4]; };
+
+__device__ __forceinline__ bool fill_window(const PagedAttnArgs& a, const Item& it, Window& win, int e0) {
+  const int n = (it.klim + (1 << a.kv.page_shift) - 1) >> a.kv.page_shift;
+  bool bad = false;
+#pragma unroll
+  for (int i = threadIdx.x; i < PW; i += 256) {
+    long off = -1;
+    if (e0 + i < n) {
+      off = page_offset(a, it.pages[e0 + i], it.g);
+      bad |= off < 0;
+      off = off < 0 ? -1 : off * 2;
+    }
+    win.off[i] = off;
+  }
+  const bool any = __ballot(bad) != 0;
+  if ((threadIdx.x & 63) == 0) win.flag[threadIdx.x >> 6] = any;
+  __syncthreads();
+  return (win.flag[0] | win.flag[1] | win.flag[2] | win.flag[3]) != 0;
+}
+
+// ---------------------------------------------------------------- bf16, waves split the rows
+// 128 rows a block, 32 a wave; the block's waves load each key tile together
+// into a ring of two. (K and V of 64 keys; 32 at head dim 256.)
+template <int HDP, bool CAP>
+__global__ void __launch_bounds__(256, 2) paged_rows_kernel(PagedAttnArgs a) {
+  using Y = Lay<HDP>;
+  constexpr int KT = HDP == 256 ? 32 : 64, NS = KT / 32, NC = HDP / 16, ND = HDP / 32;
+  constexpr int TILE = KT * Y::ROWB, IW = TILE / 4096;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * 2 * TILE];
+  __shared__ Window win;
+  Item it;
+  if (!find_item<128, KT, 1>(a, it)) return;
+  const bool direct = a.direct && it.nranges <= 1;
+  if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
+    if (!direct) empty_range<128>(a, it);
+    return;
+  }
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 31, h = lane >> 5, hd = a.kv.hd, shift = a.kv.page_shift;
+  const int wrow = it.row0 + wave * 32;
+  const bool active = wrow < it.nrows;
+  const Row w = row_of(a, it, wrow + lq);
+  const WaveLimits wl = wave_limits<32>(a, w.lim);
+  bf16x8 qf[NC];
+  {
+    const bf16* qp = reinterpret_cast<const bf16*>(a.q) + (long)w.tok * a.q_ts + (long)w.head * a.q_hs;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) qf[c] = 16 * c + 8 * h < hd ? *reinterpret_cast<const bf16x8*>(qp + 16 * c + 8 * h) : bf16x8{};
+  }
+  Acc<HDP> s;
+#pragma unroll
+  for (int u = 0; u < ND; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s.o[u][i] = 0.f;
+  s.m = -INFINITY;
+  s.l = 0.f;
+  const float sl2 = a.scale * LOG2E, c1 = CAP ? 2.f * sl2 / a.cap : 0.f, c2 = a.cap * LOG2E;
+
+  auto first_key = [&](int u) { return a.klo + (u < it.n1 ? u : u - it.n1 + it.t2) * KT; };
+  const char *kb = reinterpret_cast<const char*>(a.kv.k), *vb = reinterpret_cast<const char*>(a.kv.v);
+  const char* Z = reinterpret_cast<const char*>(zero_piece);
+  const unsigned ts2 = (unsigned)(a.kv.tok_stride * 2), smask = (1u << shift) - 1;
+  int w0 = 0;
+  bool holes = false;
+  auto window = [&](int k0) {                  // (block-uniform; a barrier has passed since the last use)
+    const int e0 = k0 >> shift, e1 = max(k0, min(k0 + KT, it.klim) - 1) >> shift;
+    if (e0 >= w0 && e1 < w0 + PW) return;
+    w0 = e0;
+    holes |= fill_window(a, it, win, w0);
+  };
+  auto issue = [&](int k0, unsigned dst) {
+#pragma unroll
+    for (int i = 0; i < IW; ++i) {
+      const int u = (i * 4 + wave) * 64 + lane, row = u / Y::CR, c = (u % Y::CR) ^ Y::swz(row), kk = k0 + row;
+      const long off = win.off[(min(kk, it.klim - 1) >> shift) - w0];
+      const long at = off + (unsigned long)(kk & smask) * ts2 + c * 16;
+      const bool ok = (kk < it.klim) & (c * 8 < hd) & (off >= 0);
+      const char *ks = ok ? kb + at : Z, *vs = ok ? vb + at : Z;
+      dma16(ks, dst + (i * 4 + wave) * 1024);
+      dma16(vs, dst + TILE + (i * 4 + wave) * 1024);
+    }
+  };
+  if (it.ubeg < it.uend) {
+    w0 = first_key(it.ubeg) >> shift;
+    holes = fill_window(a, it, win, w0);
+    issue(first_key(it.ubeg), lds_addr(smem));
+  }
+  hold(qf);
+  for (int u = it.ubeg; u < it.uend; ++u) {
+    // this tile has landed, and every wave is done with the tile before
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    char* Kt = smem + ((u - it.ubeg) & 1) * 2 * TILE;
+    const int k0 = first_key(u);
+    if (u + 1 < it.uend) {
+      window(first_key(u + 1));
+      issue(first_key(u + 1), lds_addr(smem) + ((u + 1 - it.ubeg) & 1) * 2 * TILE);
+    }
+    if (!active || tile_unseen(wl, k0, k0 + KT)) continue;
+    f32x16 sc[NS];
+#pragma unroll
+    for (int st = 0; st < NS; ++st) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[st][i] = 0.f;
+      const int row = st * 32 + lq;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(Kt + row * Y::ROWB + (((2 * c + h) ^ Y::swz(row)) << 4));
+        sc[st] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[c], sc[st], 0, 0, 0);
+      }
+    }
+    softmax_tile<HDP, NS, CAP>(s, sc, sl2, c1, c2, !holes && tile_full(wl, k0, k0 + KT), w.lim, k0, a, it, holes);
+    unsigned ad[4];
+    vt_addresses<HDP>(lds_addr(Kt + TILE), ad);
+#pragma unroll
+    for (int c = 0; c < KT / 16; ++c) {
+      const bf16x8 p = weights_of(sc[c / 2], c % 2);
+#pragma unroll
+      for (int u2 = 0; u2 < ND; ++u2)
+        s.o[u2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_vt<HDP>(ad, u2, c * 16 * Y::ROWB), p, s.o[u2], 0, 0, 0);
+    }
+  }
+  if (!active) return;
+  s.l = sum_x32(s.l);
+  repair<HDP, CAP>(a, it, s, qf, w.lim, sl2, c1, c2, max(0, it.uend - it.ubeg), KT,
+                   [&](int n) { return first_key(it.ubeg + n); });
+  if (wrow + lq >= it.nrows) return;
+  const float inv = inverse(s.l);
+#pragma unroll
+  for (int u = 0; u < ND; ++u)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      put(a, it, w, direct, 32 * u + 8 * q + 4 * h, f32x4{s.o[u][4 * q], s.o[u][4 * q + 1], s.o[u][4 * q + 2], s.o[u][4 * q + 3]}, inv);
+  if (h == 0) put_stats(a, it, w, direct, s.m, s.l);
+}
+
+// ---------------------------------------------------------------- bf16, waves split the keys
+// 32 rows a block; wave w takes every fourth tile of 32 keys into a K and a V
+// slot of its own and waits for its own loads only: no barrier in the loop, and
+// a slot is loaded again as soon as its fragments are in registers. The waves'
+// (max, sum, output) meet in LDS at the end. For single tokens, whose time is
+// that of the keys' and values' bytes.
+template <int HDP, bool CAP>
+__global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(PagedAttnArgs a) {
+  using Y = Lay<HDP>;
+  constexpr int KT = 32, NW = 4, NC = HDP / 16, ND = HDP / 32, TILE = KT * Y::ROWB, LK = TILE / 1024;
+  __shared__ __attribute__((aligned(1024))) char smem[NW * 2 * TILE];
+  __shared__ Window win;
+  __shared__ float stats[NW][32][2];
+  static_assert(NW * 2 * TILE == NW * 64 * ND * 64, "the waves' outputs fill the slots");
+  Item it;
+  if (!find_item<32, KT, NW>(a, it)) return;
+  const bool direct = a.direct && it.nranges <= 1;
+  if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
+    if (!direct) empty_range<32>(a, it);
+    return;
+  }
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 31, h = lane >> 5, hd = a.kv.hd, shift = a.kv.page_shift;
+  const Row w = row_of(a, it, it.row0 + lq);
+  const WaveLimits wl = wave_limits<32>(a, w.lim);
+  bf16x8 qf[NC];
+  {
+    const bf16* qp = reinterpret_cast<const bf16*>(a.q) + (long)w.tok * a.q_ts + (long)w.head * a.q_hs;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) qf[c] = 16 * c + 8 * h < hd ? *reinterpret_cast<const bf16x8*>(qp + 16 * c + 8 * h) : bf16x8{};
+  }
+  Acc<HDP> s;
+#pragma unroll
+  for (int u = 0; u < ND; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s.o[u][i] = 0.f;
+  s.m = -INFINITY;
+  s.l = 0.f;
+  const float sl2 = a.scale * LOG2E, c1 = CAP ? 2.f * sl2 / a.cap : 0.f, c2 = a.cap * LOG2E;
+  auto first_key = [&](int u) { return a.klo + (u < it.n1 ? u : u - it.n1 + it.t2) * KT; };
+  const char *kb = reinterpret_cast<const char*>(a.kv.k), *vb = reinterpret_cast<const char*>(a.kv.v);
+  const char* Z = reinterpret_cast<const char*>(zero_piece);
+  const unsigned ts2 = (unsigned)(a.kv.tok_stride * 2), smask = (1u << shift) - 1;
+  int w0 = 0;
+  bool holes = false;
+  char *slot_k = smem + wave * 2 * TILE, *slot_v = slot_k + TILE;
+  auto issue = [&](int k0, const char* base, unsigned dst) {
+#pragma unroll
+    for (int i = 0; i < LK; ++i) {
+      const int u = i * 64 + lane, row = u / Y::CR, c = (u % Y::CR) ^ Y::swz(row), kk = k0 + row;
+      // (keys behind the last read the entry of the last, or the window's first)
+      const long off = win.off[max(0, (min(kk, it.klim - 1) >> shift) - w0)];
+      const bool ok = (kk < it.klim) & (c * 8 < hd) & (off >= 0);
+      const char* p = ok ? base + (off + (unsigned long)(kk & smask) * ts2 + c * 16) : Z;
+      dma16(p, dst + i * 1024);
+    }
+  };
+  const int nrounds = (it.uend - it.ubeg + NW - 1) / NW;
+  if (nrounds > 0) {
+    w0 = first_key(it.ubeg) >> shift;
+    holes = fill_window(a, it, win, w0);
+    if (it.ubeg + wave < it.uend) {
+      issue(first_key(it.ubeg + wave), kb, lds_addr(slot_k));
+      issue(first_key(it.ubeg + wave), vb, lds_addr(slot_v));
+    }
+  }
+  unsigned ad[4];
+  vt_addresses<HDP>(lds_addr(slot_v), ad);
+  hold(qf);
+#pragma unroll 1
+  for (int p = 0; p < nrounds; ++p) {
+    const int u = it.ubeg + p * NW + wave, k0 = first_key(u);
+    const bool next = u + NW < it.uend;
+    if (p + 1 < nrounds) {                     // the next round's pages (block-uniform)
+      const int n0 = first_key(it.ubeg + (p + 1) * NW), e0 = n0 >> shift,
+                e1 = max(n0, min(n0 + NW * KT, it.klim) - 1) >> shift;
+      if (e0 < w0 || e1 >= w0 + PW) {
+        __syncthreads();
+        w0 = e0;
+        holes |= fill_window(a, it, win, w0);
+      }
+    }
+    if (u >= it.uend) continue;
+    // this tile's keys have landed once only its values' loads are pending
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LK) : "memory");
+    bf16x8 kf[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      kf[c] = *reinterpret_cast<const bf16x8*>(slot_k + lq * Y::ROWB + (((2 * c + h) ^ Y::swz(lq)) << 4));
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    if (next) issue(first_key(u + NW), kb, lds_addr(slot_k));
+    f32x16 sc[1];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[0][i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], qf[c], sc[0], 0, 0, 0);
+    softmax_tile<HDP, 1, CAP>(s, sc, sl2, c1, c2, !holes && tile_full(wl, k0, k0 + KT), w.lim, k0, a, it, holes);
+    // the values have landed once only the next keys' loads are pending
+    if (next) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LK) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    bf16x8 vf[2][ND];
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int u2 = 0; u2 < ND; ++u2) vf[c][u2] = read_vt<HDP>(ad, u2, c * 16 * Y::ROWB);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    if (next) issue(first_key(u + NW), vb, lds_addr(slot_v));
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const bf16x8 pf = weights_of(sc[0], c);
+#pragma unroll
+      for (int u2 = 0; u2 < ND; ++u2) s.o[u2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c][u2], pf, s.o[u2], 0, 0, 0);
+    }
+  }
+  s.l = sum_x32(s.l);
+  {
+    const int mine = it.uend - it.ubeg - wave;
+    repair<HDP, CAP>(a, it, s, qf, w.lim, sl2, c1, c2, mine > 0 ? (mine + NW - 1) / NW : 0, KT,
+                     [&](int n) { return first_key(it.ubeg + n * NW + wave); });
+  }
+  // the waves store outputs and statistics, then each adds a quarter of the dims in wave order
+  __syncthreads();
+  f32x4* mo = reinterpret_cast<f32x4*>(smem);
+#pragma unroll
+  for (int u = 0; u < ND; ++u)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      mo[(wave * ND * 4 + u * 4 + q) * 64 + lane] = f32x4{s.o[u][4 * q], s.o[u][4 * q + 1], s.o[u][4 * q + 2], s.o[u][4 * q + 3]};
+  if (h == 0) {
+    stats[wave][lq][0] = s.m;
+    stats[wave][lq][1] = s.l;
+  }
+  __syncthreads();
+  float m = -INFINITY, l = 0.f, wt[NW];
+#pragma unroll
+  for (int q = 0; q < NW; ++q) m = vmax(m, stats[q][lq][0]);
+#pragma unroll
+  for (int q = 0; q < NW; ++q) {
+    // (a wave without keys weighs nothing)
+    wt[q] = stats[q][lq][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stats[q][lq][0] - m);
+    l += stats[q][lq][1] * wt[q];
+  }
+  if (it.row0 + lq >= it.nrows) return;
+  const float inv = inverse(l);
+#pragma unroll
+  for (int i = 0; i < ND; ++i) {
+    const int j = wave * ND + i;               // f32x4 j of the lane: subtile j / 4, group j % 4
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int q = 0; q < NW; ++q) {
+      const f32x4 x = mo[(q * ND * 4 + j) * 64 + lane];
+      if (wt[q] != 0.f) acc += x * wt[q];
+    }
+    put(a, it, w, direct, 32 * (j / 4) + 8 * (j % 4) + 4 * h, acc, inv);
+  }
+  if (wave == 0 && h == 0) put_stats(a, it, w, direct, m, l);
+}
+
+// ---------------------------------------------------------------- fp32
+// 16 rows a block, eight waves split the tiles of 16 keys; both products on
+// v_mfma_f32_16x16x4_f32 with operands straight from global memory. A tile's
+// page numbers are requested while the tile before is computed.
+template <int HDP, bool CAP>
+__global__ void __launch_bounds__(512) paged_f32_kernel(PagedAttnArgs a) {
+  constexpr int NW = 8, KT = 16, NC = HDP / 16, REC = HDP / 4 + 4;
+  __shared__ __attribute__((aligned(16))) float mg[NW / 2][64 * REC];
+  Item it;
+  if (!find_item<16, KT, 1>(a, it)) return;
+  const bool direct = a.direct && it.nranges <= 1;
+  if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
+    if (!direct) empty_range<16>(a, it);
+    return;
+  }
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 15, lk = lane >> 4, hd = a.kv.hd, shift = a.kv.page_shift, smask = (1 << shift) - 1;
+  const Row w = row_of(a, it, it.row0 + lr);
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  const float* qp = reinterpret_cast<const float*>(a.q) + (long)w.tok * a.q_ts + (long)w.head * a.q_hs;
+  f32x4 qf[NC], o[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    qf[c] = c * 16 + lk * 4 < hd ? *reinterpret_cast<const f32x4*>(qp + c * 16 + lk * 4) : zero;
+    o[c] = zero;
+  }
+  float m = -INFINITY, l = 0.f;
+  auto first_key = [&](int u) { return a.klo + (u < it.n1 ? u : u - it.n1 + it.t2) * KT; };
+  auto page_at = [&](int j) { return it.pages[min(j, it.klim - 1) >> shift]; };
+  const float *kb = reinterpret_cast<const float*>(a.kv.k), *vb = reinterpret_cast<const float*>(a.kv.v);
+  // the score of a dot product; exact functions, the sums' errors are of their size
+  auto score = [&](float d) { return CAP ? a.cap * tanhf(d * a.scale / a.cap) : d * a.scale; };
+  int pk = 0, pv[4] = {0, 0, 0, 0};
+  auto request = [&](int u) {
+    const int k0 = first_key(u);
+    pk = page_at(k0 + lr);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) pv[e] = page_at(k0 + 4 * lk + e);
+  };
+  if (it.ubeg + wave < it.uend) request(it.ubeg + wave);
+#pragma unroll 1
+  for (int u = it.ubeg + wave; u < it.uend; u += NW) {
+    const int k0 = first_key(u);
+    const long ko = page_offset(a, pk, it.g) + (long)((k0 + lr) & smask) * a.kv.tok_stride;
+    const bool kok = (unsigned)pk < (unsigned)a.kv.n_pages && k0 + lr < it.klim;
+    long vo[4];
+    bool vok[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = k0 + 4 * lk + e;
+      vok[e] = (unsigned)pv[e] < (unsigned)a.kv.n_pages && j < it.klim;
+      vo[e] = page_offset(a, pv[e], it.g) + (long)(j & smask) * a.kv.tok_stride;
+    }
+    f32x4 kf[NC], vf[NC];                      // vf[c][e]: V[key 4 lk + e][16 c + lr]
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      kf[c] = kok && c * 16 + lk * 4 < hd ? *reinterpret_cast<const f32x4*>(kb + ko + c * 16 + lk * 4) : zero;
+    auto load_v = [&]() {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) vf[c][e] = vok[e] && c * 16 + lr < hd ? vb[vo[e] + c * 16 + lr] : 0.f;
+    };
+    if constexpr (HDP <= 128) load_v();        // (at 256 both would not fit the registers)
+    if (u + NW < it.uend) request(u + NW);
+    f32x4 sc = zero;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c][e], qf[c][e], sc, 0, 0, 0);
+    if constexpr (HDP > 128) load_v();
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      sc[e] = vok[e] && sees(w.lim, k0 + 4 * lk + e) ? score(sc[e]) : -INFINITY;
+      mx = vmax(mx, sc[e]);
+    }
+    mx = vmax(mx, __shfl_xor(mx, 16));
+    mx = vmax(mx, __shfl_xor(mx, 32));
+    const float mn = vmax(m, mx), ref = mn == -INFINITY ? 0.f : mn, alpha = __expf(m - ref);
+    float ps = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      sc[e] = __expf(sc[e] - ref);
+      ps += sc[e];
+    }
+    l = l * alpha + ps;
+    m = mn;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      o[c] *= alpha;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[c][e], sc[e], o[c], 0, 0, 0);
+    }
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  // rows with an output that is not finite: again, key by key (as `repair`)
+  float z = 0.f;
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z = __builtin_fmaf(o[c][e], 0.f, z);
+  if (__ballot(z != z) != 0) {
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) o[c] = zero;
+#pragma unroll 1
+    for (int u = it.ubeg + wave; u < it.uend; u += NW) {
+      const int k0 = first_key(u);
+#pragma unroll 1
+      for (int j = k0; j < min(k0 + KT, it.klim); ++j) {
+        const bool vis = sees(w.lim, j);
+        if (__ballot(vis) == 0) continue;
+        const long off = page_offset(a, it.pages[j >> shift], it.g);
+        if (off < 0) continue;
+        const long at = off + (long)(j & smask) * a.kv.tok_stride;
+        float d = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          if (c * 16 + lk * 4 < hd) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(kb + at + c * 16 + lk * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d = __builtin_fmaf(x[e], qf[c][e], d);
+          }
+        d += __shfl_xor(d, 16);
+        d += __shfl_xor(d, 32);
+        const float p = __expf(score(d) - ref);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          if (vis && c * 16 + lk * 4 < hd) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(vb + at + c * 16 + lk * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c][e] = __builtin_fmaf(p, x[e], o[c][e]);
+          }
+      }
+    }
+  }
+  // merge the waves, the upper half into the lower until wave 0 holds all
+  for (int n = NW / 2; n > 0; n /= 2) {
+    if (wave >= n && wave < 2 * n) {
+      float* dst = mg[wave - n] + lane * REC;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) *reinterpret_cast<f32x4*>(dst + 4 * c) = o[c];
+      dst[HDP / 4] = m;
+      dst[HDP / 4 + 1] = l;
+    }
+    __syncthreads();
+    if (wave < n) {
+      const float* src = mg[wave] + lane * REC;
+      const float m2 = src[HDP / 4], l2 = src[HDP / 4 + 1], mm = vmax(m, m2);
+      // (a wave without keys weighs nothing)
+      const float w1 = m == -INFINITY ? 0.f : __expf(m - mm), w2 = m2 == -INFINITY ? 0.f : __expf(m2 - mm);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(src + 4 * c);
+        if (w1 != 1.f) o[c] = w1 == 0.f ? zero : o[c] * w1;
+        if (w2 != 0.f) o[c] += x * w2;
+      }
+      l = l * w1 + l2 * w2;
+      m = mm;
+    }
+    __syncthreads();
+  }
+  if (wave != 0 || it.row0 + lr >= it.nrows) return;
+  const float inv = inverse(l);
+  const long row = (long)w.tok * a.n_q + w.head;
+  float* op = direct ? reinterpret_cast<float*>(a.o) + (long)w.tok * a.o_ts + (long)w.head * a.o_hs : part_of(a, row, it.slot);
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+    if (c * 16 + lk * 4 < hd) *reinterpret_cast<f32x4*>(op + c * 16 + lk * 4) = direct ? o[c] * inv : o[c];
+  if (lk != 0) return;
+  if (!direct) {
+    store_stats(a, row, it.slot, m * LOG2E, l);
+  } else {
+    if (a.lse) a.lse[row] = m + logf(l);
+    if (a.slots > 1) store_stats(a, row, 0, 0.f, -1.f);
+  }
+}
+
+// ---------------------------------------------------------------- merge of ranges
+// One block a row: its four waves take every fourth slot, their sums meet in
+// LDS in wave order. A lane owns four dims.
+template <typename T>
+__global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a) {
+  __shared__ float st[4][2];
+  __shared__ __attribute__((aligned(16))) f32x4 acc[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, S = a.slots, hd = a.kv.hd;
+  const int tok = blockIdx.x, head = blockIdx.y;
+  const long row = (long)tok * a.n_q + head;
+  if (tok < a.bt.start[0] || tok >= a.bt.start[a.bt.n_req]) return;
+  const float* stat = a.ws + (long)a.bt.n_tok * a.n_q * S * hd + row * S * 2;
+  if (stat[1] < 0.f) return;                   // written already
+  float m = -INFINITY;
+  for (int i = lane; i < S; i += 64) m = vmax(m, stat[2 * i + 1] == 0.f ? -INFINITY : stat[2 * i]);
+  for (int o = 32; o > 0; o >>= 1) m = vmax(m, __shfl_xor(m, o));
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+#pragma unroll 4
+  for (int i = wave; i < S; i += 4) {
+    const float ms = stat[2 * i], ls = stat[2 * i + 1];
+    if (ls == 0.f) continue;                   // (no keys; a NaN sum is not 0)
+    const float w = __builtin_amdgcn_exp2f(ms - m);
+    l += ls * w;
+    if (lane * 4 < hd) s += *reinterpret_cast<const f32x4*>(part_of(a, row, i) + lane * 4) * w;
+  }
+  if (lane == 0) st[wave][0] = l;
+  acc[wave][lane] = s;
+  __syncthreads();
+  if (wave != 0) return;
+  l = (st[0][0] + st[1][0]) + (st[2][0] + st[3][0]);
+  s = (acc[0][lane] + acc[1][lane]) + (acc[2][lane] + acc[3][lane]);
+  const float inv = inverse(l);
+  if (lane * 4 < hd) {
+    T* op = reinterpret_cast<T*>(a.o) + (long)tok * a.o_ts + (long)head * a.o_hs + lane * 4;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x4*>(op) = bf16x4{(bf16)(s[0] * inv), (bf16)(s[1] * inv), (bf16)(s[2] * inv), (bf16)(s[3] * inv)};
+    else *reinterpret_cast<f32x4*>(op) = s * inv;
+  }
+  if (a.lse && lane == 0) a.lse[row] = m * LN2 + logf(l);
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------- host
+// Rows of a tile and keys of a key tile of kernel k at padded head dim hdp.
+static int tile_rows(int k) { return k == 0 ? 32 : k == 1 ? 128 : 16; }
+static int tile_keys(int k, int hdp) { return k == 0 ? 32 : k == 1 ? (hdp == 256 ? 32 : 64) : 16; }
+
+// Key ranges of a part: enough blocks for two a CU, ranges of 2048 keys at
+// most for single tokens (requests differ in length: short ranges share the
+// work evenly), of 256 at least.
+static void cut(PagedPart& p, int hdp, int keys, int n_kv) {
+  const int kt = tile_keys(p.kernel, hdp), unit = p.kernel == 0 ? 4 : 1;   // (lists are padded to whole units)
+  auto up = [](long x, long m) { return (x + m - 1) / m * m; };
+  const long total = up(std::max(1, (keys + kt - 1) / kt), unit), blocks = (long)p.tiles * n_kv;
+  long want = (512 + blocks - 1) / blocks;
+  if (p.kernel == 0) want = std::max<long>(want, (keys + 2047) / 2048);
+  long per = up(std::max<long>(256 / kt, (total + want - 1) / want), unit);
+  per = std::max(per, up((total + 65534) / 65535, unit));                  // (the grid's second extent)
+  p.chunk = (int)per;
+  p.ranges = (int)((total + per - 1) / per);
+}
+
+PagedPlan paged_plan(const PagedAttnArgs& a, int et) {
+  PagedPlan p{};
+  p.hdp = a.kv.hd <= 64 ? 64 : a.kv.hd <= 128 ? 128 : 256;
+  auto part = [&](long rows_req, bool flat, int keys) {
+    PagedPart q{};
+    const long rows = flat ? (long)a.bt.n_tok * a.G : rows_req;
+    q.kernel = et == ET_F32 ? 2 : rows <= 32 ? 0 : 1;
+    const int br = tile_rows(q.kernel);
+    const long all = (long)a.bt.n_tok * a.G;
+    q.tiles = (int)(flat ? std::max<long>(1, (all + br - 1) / br) : rows_req <= br ? a.bt.n_req : all / br + a.bt.n_req);
+    cut(q, p.hdp, keys, a.kv.n_kv);
+    return q;
+  };
+  const long rows_req = (long)a.bt.max_new * a.G;
+  if (a.shared_len > 0) {
+    p.n_parts = 2;
+    p.part[0] = part(rows_req, true, a.shared_len);
+    p.part[1] = part(rows_req, false, a.bt.max_len - a.shared_len);
+    p.slots = p.part[0].ranges + p.part[1].ranges;
+  } else {
+    p.n_parts = 1;
+    p.part[0] = part(rows_req, false, a.bt.max_len);
+    p.slots = p.part[0].ranges;
+  }
+  return p;
+}
+
+size_t paged_attention_ws(const PagedAttnArgs& a, int et) {
+  const PagedPlan p = paged_plan(a, et);
+  return p.slots > 1 ? (size_t)a.bt.n_tok * a.n_q * p.slots * (a.kv.hd + 2) * 4 : 0;
+}
+
+template <int HDP, bool CAP>
+static void launch_part(const PagedAttnArgs& a, int kernel, hipStream_t s) {
+  const dim3 grid((unsigned)a.tiles * a.kv.n_kv, a.ranges);
+  if (kernel == 0) hipLaunchKernelGGL((paged_keys_kernel<HDP, CAP>), grid, dim3(256), 0, s, a);
+  else if (kernel == 1) hipLaunchKernelGGL((paged_rows_kernel<HDP, CAP>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP>), grid, dim3(512), 0, s, a);
+}
+
+void launch_paged_attention(const PagedAttnArgs& a, int et, hipStream_t s) {
+  if (a.bt.n_tok <= 0 || a.bt.max_new <= 0) return;
+  const PagedPlan p = paged_plan(a, et);
+  int slot = 0;
+  for (int i = 0; i < p.n_parts; ++i) {
+    const PagedPart& q = p.part[i];
+    PagedAttnArgs b = a;
+    b.flat = p.n_parts == 2 && i == 0;
+    b.klo = p.n_parts == 2 && i == 1 ? a.shared_len : 0;
+    b.khi = b.flat ? a.shared_len : 1 << 30;
+    b.tiles = q.tiles; b.chunk = q.chunk; b.ranges = q.ranges;
+    b.slot0 = slot; b.slots = p.slots;
+    b.direct = p.n_parts == 1;
+    slot += q.ranges;
+    const bool cap = a.cap > 0.f;
+    if (p.hdp == 64) cap ? launch_part<64, true>(b, q.kernel, s) : launch_part<64, false>(b, q.kernel, s);
+    else if (p.hdp == 128) cap ? launch_part<128, true>(b, q.kernel, s) : launch_part<128, false>(b, q.kernel, s);
+    else cap ? launch_part<256, true>(b, q.kernel, s) : launch_part<256, false>(b, q.kernel, s);
+  }
+  if (p.slots > 1) {
+    PagedAttnArgs b = a;
+    b.slots = p.slots;
+    const dim3 grid(a.bt.n_tok, a.n_q);
+    if (et == ET_BF16) hipLaunchKernelGGL(paged_merge_kernel<bf16>, grid, dim3(256), 0, s, b);
+    else hipLaunchKernelGGL(paged_merge_kernel<float>, grid, dim3(256), 0, s, b);
+  }
+}

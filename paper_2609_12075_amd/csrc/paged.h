@@ -37,9 +37,27 @@ struct PagedAttnArgs {
   float scale, cap;
   int causal, window;
   const int32_t* prefix;
-  int shared_len;                              // keys below it: pages of request 0
+  int shared_len;                              // keys below it lie on the pages of request 0
+  // Scratch: unnormalised outputs [n_tok][n_q][slots][hd], then (max in log2
+  // units, sum) pairs [n_tok][n_q][slots], fp32. A sum of -1 in slot 0: the
+  // row's output is written already.
   float* ws;
+  // set by the launcher, per launch
+  int klo, khi;                                // keys [klo, khi) only
+  int flat;                                    // rows of the whole batch in one sequence of tiles, pages of request 0
+  int tiles;                                   // row tiles of the grid
+  int chunk;                                   // key tiles per range
+  int ranges, slot0, slots;                    // ranges of this launch, its first slot, slots of a row
+  int direct;                                  // rows whose keys fit one range are written at once
 };
+
+// How an attention is computed. kernel 0: a block owns 32 rows (token, query
+// head of the group), its waves split the keys; 1: its waves split 128 rows; 2:
+// fp32, 16 rows. One part over the cache, or two: the common context (all rows
+// of the batch in one sequence of tiles) and what follows it.
+struct PagedPart { int kernel, tiles, chunk, ranges; };
+struct PagedPlan { int n_parts, hdp, slots; PagedPart part[2]; };
+PagedPlan paged_plan(const PagedAttnArgs& a, int et);
 size_t paged_attention_ws(const PagedAttnArgs& a, int et);
 void launch_paged_attention(const PagedAttnArgs& a, int et, hipStream_t s);
 
@@ -79,6 +97,19 @@ __device__ __forceinline__ int request_of(const RaggedBatch& b, int tok) {
     const int end = lo + n;
     lo += last * step;
     n = end - lo < step ? end - lo : step;
+  }
+  return lo;
+}
+
+// The same for a token of each lane's own.
+__device__ __forceinline__ int lane_request_of(const RaggedBatch& b, int tok) {
+  // one token a request is the usual batch
+  if (tok < b.n_req && b.start[tok] <= tok && tok < b.start[tok + 1]) return tok;
+  int lo = 0, hi = b.n_req;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (b.start[mid] <= tok) lo = mid;
+    else hi = mid;
   }
   return lo;
 }

@@ -1,5 +1,6 @@
 // C ABI of the paged key/value cache (include/vla_paged.h): argument checks,
 // and the launches on the pool's device.
+#include <algorithm>
 #include <cmath>
 #include <new>
 
@@ -46,7 +47,7 @@ void check_rows(const void* p, int64_t ts, int64_t hs, int rows, int heads, int 
 void fill(const vla_kv_pool* p, const vla_ragged* b, bool buffers, PagedKV& kv, RaggedBatch& bt) {
   VLA_REQUIRE(p && b, "null pool or batch");
   VLA_REQUIRE(p->dtype == VLA_F32 || p->dtype == VLA_BF16, "pool dtype must be VLA_F32 or VLA_BF16");
-  VLA_REQUIRE(p->n_kv >= 1 && p->n_kv <= 65535, "n_kv must be in [1, 65535]");
+  VLA_REQUIRE(p->n_kv >= 1 && p->n_kv <= 4096, "n_kv must be in [1, 4096]");
   VLA_REQUIRE(p->head_dim >= 8 && p->head_dim <= 256 && p->head_dim % 8 == 0, "head_dim must be a multiple of 8 in [8, 256]");
   VLA_REQUIRE(p->page_tokens >= 1 && p->page_tokens <= 65536 && (p->page_tokens & (p->page_tokens - 1)) == 0,
               "page_tokens must be a power of two in [1, 65536]");
@@ -60,6 +61,7 @@ void fill(const vla_kv_pool* p, const vla_ragged* b, bool buffers, PagedKV& kv, 
   check_stride(p->page_stride, p->n_pages, p->head_dim, es, "pool page");
   check_stride(p->head_stride, p->n_kv, p->head_dim, es, "pool head");
   check_stride(p->token_stride, p->page_tokens, p->head_dim, es, "pool token");
+  VLA_REQUIRE(p->page_tokens == 1 || p->token_stride * es < (1LL << 31), "pool token stride must be below 2^31 bytes");
   if (buffers) {
     VLA_REQUIRE(p->k && p->v && aligned(p->k, 16) && aligned(p->v, 16), "pool k and v must be 16-byte aligned buffers");
     VLA_REQUIRE(b->start && b->kv_len && (b->pages || b->pages_stride == 0), "null start, kv_len or pages");
@@ -82,7 +84,7 @@ PagedAttnArgs attention_args(const vla_kv_pool* p, const vla_ragged* b, const vl
   PagedAttnArgs a{};
   // (the host's own checks first, so that a refusal needs no GPU)
   fill(p, b, false, a.kv, a.bt);
-  VLA_REQUIRE(t->n_q >= 1 && t->n_q <= 65535 && t->n_q % p->n_kv == 0, "n_q must be a multiple of n_kv in [1, 65535]");
+  VLA_REQUIRE(t->n_q >= 1 && t->n_q <= 4096 && t->n_q % p->n_kv == 0, "n_q must be a multiple of n_kv in [1, 4096]");
   VLA_REQUIRE((long)b->n_tok * t->n_q < (1L << 30), "n_tok * n_q must be below 2^30");
   VLA_REQUIRE(t->scale >= 0.f && std::isfinite(t->scale), "scale must be positive, or 0 for 1 / sqrt(head_dim)");
   VLA_REQUIRE(t->cap >= 0.f && std::isfinite(t->cap), "cap must be >= 0");
@@ -103,7 +105,7 @@ PagedAttnArgs attention_args(const vla_kv_pool* p, const vla_ragged* b, const vl
   a.q_ts = t->q_tok_stride; a.q_hs = t->q_head_stride; a.o_ts = t->o_tok_stride; a.o_hs = t->o_head_stride;
   a.lse = t->lse; a.n_q = t->n_q; a.G = t->n_q / p->n_kv;
   a.scale = t->scale > 0.f ? t->scale : 1.0f / std::sqrt((float)p->head_dim);
-  a.cap = t->cap; a.causal = t->causal; a.window = t->window; a.prefix = t->prefix;
+  a.cap = t->cap; a.causal = t->causal; a.window = std::min(t->window, 1 << 30); a.prefix = t->prefix;
   a.shared_len = shared_len;
   a.ws = static_cast<float*>(t->ws);
   return a;
@@ -134,7 +136,7 @@ vla_status vla_kv_append(const vla_kv_pool* p, const vla_ragged* b, const vla_ap
     const int es = (int)elem_size(p->dtype), rows = b->n_tok, hd = p->head_dim;
     check_rows(t->k, t->k_tok_stride, t->k_head_stride, rows, p->n_kv, hd, es, "k");
     check_rows(t->v, t->v_tok_stride, t->v_head_stride, rows, p->n_kv, hd, es, "v");
-    VLA_REQUIRE(t->n_q >= 0 && t->n_q <= 65535, "n_q must be in [0, 65535]");
+    VLA_REQUIRE(t->n_q >= 0 && t->n_q <= 4096, "n_q must be in [0, 4096]");
     if (t->n_q > 0) {
       check_rows(t->q, t->q_tok_stride, t->q_head_stride, rows, t->n_q, hd, es, "q");
       check_rows(t->q_out, t->qo_tok_stride, t->qo_head_stride, rows, t->n_q, hd, es, "q_out");
@@ -172,6 +174,19 @@ vla_status vla_attention_workspace(const vla_kv_pool* p, const vla_ragged* b, co
   return guarded([&] {
     VLA_REQUIRE(bytes != nullptr, "null bytes");
     *bytes = paged_attention_ws(attention_args(p, b, t, shared_len != 0, shared_len, false), p->dtype);
+  });
+}
+
+vla_status vla_debug_paged_plan(const vla_kv_pool* p, const vla_ragged* b, const vla_attention_args* t, int shared_len,
+                                int* plan) {
+  return guarded([&] {
+    VLA_REQUIRE(plan != nullptr, "null plan");
+    const PagedPlan q = paged_plan(attention_args(p, b, t, shared_len != 0, shared_len, false), p->dtype);
+    plan[0] = q.hdp;
+    for (int i = 0; i < 2; ++i) {
+      const PagedPart r = i < q.n_parts ? q.part[i] : PagedPart{-1, 0, 0, 0};
+      plan[1 + 4 * i] = r.kernel; plan[2 + 4 * i] = r.tiles; plan[3 + 4 * i] = r.chunk; plan[4 + 4 * i] = r.ranges;
+    }
   });
 }
 

@@ -15,7 +15,8 @@ from typing import Optional, Sequence
 
 from . import vla
 
-EXPORTS = ["vla_kv_append", "vla_attention_workspace", "vla_paged_attention", "vla_shared_attention"]
+EXPORTS = ["vla_kv_append", "vla_attention_workspace", "vla_paged_attention", "vla_shared_attention",
+           "vla_debug_paged_plan"]
 
 _ci, _vp, _i64 = ctypes.c_int, ctypes.c_void_p, ctypes.c_int64
 
@@ -56,6 +57,7 @@ def _lib():
         L.vla_attention_workspace.argtypes = [P(KVPoolC), P(RaggedC), P(AttentionArgsC), _ci, P(ctypes.c_size_t)]
         L.vla_paged_attention.argtypes = [P(KVPoolC), P(RaggedC), P(AttentionArgsC), _vp]
         L.vla_shared_attention.argtypes = [P(KVPoolC), P(RaggedC), P(AttentionArgsC), _ci, _vp]
+        L.vla_debug_paged_plan.argtypes = [P(KVPoolC), P(RaggedC), P(AttentionArgsC), _ci, P(_ci)]
         for n in EXPORTS:
             getattr(L, n).restype = _ci
         _L = L
