@@ -15,6 +15,7 @@
 // element by element. Ranges of one tile of rows go to different blocks where
 // the rows alone would not fill the chip, and are merged by a second kernel.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.h"
 
@@ -243,28 +244,135 @@ __device__ __forceinline__ unsigned lds_addr(const void* p) {
 // compiler, which cannot tell the slots of a ring apart, waits for all of its
 // own direct loads before each LDS read; these loads' waits are in the loops.
 __device__ __forceinline__ void dma16(const void* src, unsigned dst) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(dst) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(dst) : "memory");
+}
+
+// The same from a wave-uniform base and 32-bit offsets of the lanes.
+__device__ __forceinline__ void dma16(const char* base, unsigned off, unsigned dst) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(dst) : "memory");
 }
 
 // V^T fragments of a 16-key group: subtile u (32 dims) holds, of lane l, dim
 // l % 32 of keys 4 (l / 32) + 0..3 and + 8..11: two transposing reads of four
-// keys each. ad[u]: the lane's byte address of subtile u's first read (of
-// subtiles 0 .. 3; 4 .. 7 lie 256 bytes on); off: bytes to the group.
+// keys each. at: the lane's byte address of subtile 0's first read; off: bytes
+// to the group.
 typedef short v4s __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ bf16x4 read_tr(unsigned at) {
   typedef __attribute__((address_space(3))) v4s* P;
   return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)at));
 }
 template <int HDP>
-__device__ __forceinline__ bf16x8 read_vt(const unsigned (&ad)[4], int u, int off) {
-  const bf16x4 l = read_tr(ad[u % 4] + off + u / 4 * 256),
-               h = read_tr(ad[(u % 4) ^ Lay<HDP>::HX] + off + u / 4 * 256 + 8 * Lay<HDP>::ROWB);
+__device__ __forceinline__ bf16x8 read_vt(unsigned at, int u, int off) {
+  const int hu = (u % 4) ^ Lay<HDP>::HX;
+  const bf16x4 l = read_tr((at ^ (u % 4 << 6)) + off + u / 4 * 256),
+               h = read_tr((at ^ (hu << 6)) + off + u / 4 * 256 + 8 * Lay<HDP>::ROWB);
   return __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// The lane's first byte for read_vt within a tile.
+template <int HDP>
+__device__ __forceinline__ unsigned vt_address() {
+  const int lane = threadIdx.x & 63, s = lane & 15, r = 4 * (lane >> 5) + (s >> 2);
+  const int c = 2 * ((lane >> 4) & 1) + ((s & 3) >> 1);
+  return r * Lay<HDP>::ROWB + ((c ^ Lay<HDP>::swz(r)) << 4) + ((s & 1) << 3);
+}
+// 16 bytes of a key row: 8 dims from 16 c on (and 8 of the lane half).
+__device__ __forceinline__ bf16x8 read_k(unsigned at, int c, int off) {
+  typedef const __attribute__((address_space(3))) bf16x8* P;
+  return *(P)(uintptr_t)((at ^ (c % 8 << 5)) + off + c / 8 * 256);
 }
 
 // The window of page offsets a block keeps in LDS (bytes from the pool's bases
 // of this KV head's rows; -1: not there), entries w0 .. w0 + PW - 1.
 constexpr int PW = 512;
+
+// Fills the window of page offsets from entry e0 on; true where a page that
+// the item's keys need is not there.
+// (all threads of the block call it, and none reads the window or the flags
+// of an earlier call any more; ends with a barrier)
+struct Window { long off[PW]; int flag[8]; };
+
+template <int THREADS>
+__device__ __forceinline__ bool fill_window(const PagedAttnArgs& a, const Item& it, Window& win, int e0) {
+  const int n = (it.klim + (1 << a.kv.page_shift) - 1) >> a.kv.page_shift;
+  bool bad = false;
+#pragma unroll
+  for (int i = threadIdx.x; i < PW; i += THREADS) {
+    long off = -1;
+    if (e0 + i < n) {
+      off = page_offset(a, it.pages[e0 + i], it.g);
+      bad |= off < 0;
+      off = off < 0 ? -1 : off * 2;
+    }
+    win.off[i] = off;
+  }
+  const bool any = __ballot(bad) != 0;
+  if ((threadIdx.x & 63) == 0) win.flag[threadIdx.x >> 6] = any;
+  __syncthreads();
+  int f = 0;
+#pragma unroll
+  for (int i = 0; i < THREADS / 64; ++i) f |= win.flag[i];
+  return f != 0;
+}
+
+// Moves a wave's share of a tile of KT key rows into LDS: NWV waves share a
+// tile, load j of the tile (RS rows) belongs to wave j % NWV.
+template <int HDP, int KT, int NWV>
+struct Mover {
+  using Y = Lay<HDP>;
+  static constexpr int RS = 64 / Y::CR, N = KT / RS / NWV, ROWS = N * RS;
+  unsigned lrow, piece, wave, ts2, smask;
+  int shift, hd;
+  const Window* win;
+  // where the row of each lane begins (lane l: row l % ROWS of the wave's), and whether it is there
+  long at;
+  bool ok;
+
+  __device__ __forceinline__ Mover(const PagedAttnArgs& a, const Window& w, int wv) {
+    const unsigned lane = threadIdx.x & 63;
+    lrow = lane / Y::CR;
+    piece = ((lane % Y::CR) ^ (lrow / Y::RP)) << 4;
+    wave = wv;
+    ts2 = (unsigned)(a.kv.tok_stride * 2);
+    shift = a.kv.page_shift;
+    smask = (1u << shift) - 1;
+    hd = a.kv.hd;
+    win = &w;
+  }
+  // the rows of the tile at key k0 (window from entry w0; keys from klim on are zeros)
+  __device__ __forceinline__ void rows(int k0, int w0, int klim) {
+    const int l = (threadIdx.x & 63) % ROWS, kk = k0 + (l / RS * NWV + (int)wave) * RS + l % RS;
+    const long off = win->off[max(0, (min(kk, klim - 1) >> shift) - w0)];
+    at = off + (unsigned long)(kk & smask) * ts2;
+    ok = (kk < klim) & (off >= 0);
+  }
+  template <bool BOTH>
+  __device__ __forceinline__ void load(const char* kb, const char* vb, unsigned dst_k, unsigned dst_v) const {
+    // all rows there, each load's rows in one page: bases are scalars
+    if (__ballot(ok) == ~0ull && shift >= __builtin_ctz(RS) && hd == HDP) {
+      const int lo = (int)at, hi = (int)(at >> 32);
+      const unsigned row = lrow * ts2;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const unsigned j = i * NWV + wave, off = row + (piece ^ (((j * RS / Y::RP) & Y::SWM) << 4));
+        const long b = (long)((unsigned long)(unsigned)__builtin_amdgcn_readlane(hi, i * RS) << 32 |
+                              (unsigned)__builtin_amdgcn_readlane(lo, i * RS));
+        dma16(kb + b, off, dst_k + j * 1024);
+        if constexpr (BOTH) dma16(vb + b, off, dst_v + j * 1024);
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < N; ++i) {
+        const unsigned j = i * NWV + wave, c = piece ^ (((j * RS / Y::RP) & Y::SWM) << 4);
+        const int src = i * RS + lrow;
+        const long b = __shfl(at, src) + c;
+        const bool there = __shfl((int)ok, src) & (c < 2u * hd);
+        const char* z = reinterpret_cast<const char*>(zero_piece);
+        dma16(there ? kb + b : z, dst_k + j * 1024);
+        if constexpr (BOTH) dma16(there ? vb + b : z, dst_v + j * 1024);
+      }
+    }
+  }
+};
 
 // ---------------------------------------------------------------- bf16, common
 // State of a wave: 32 rows, all dims.
@@ -310,10 +418,18 @@ __device__ __forceinline__ void softmax_tile(Acc<HDP>& s, f32x16 (&sc)[NS], floa
   for (int i = 1; i < 16 * NS; ++i) mx = vmax(mx, sc[i / 16][i % 16]);
   mx = max_x32(mx);
   if constexpr (!CAP) mx *= sl2;
-  // (rows that have seen nothing keep a reference of 0: no -inf - -inf)
-  const float mn = vmax(s.m, mx), ref = mn == -INFINITY ? 0.f : mn;
-  const float alpha = __builtin_amdgcn_exp2f(s.m - ref);
-  s.m = mn;
+  // The reference follows a row's maximum only where that grew by more than
+  // 2^8 (or the row saw its first key): the outputs are rescaled rarely then,
+  // and a weight of up to 2^8 loses nothing in fp32 or, rounded, in bf16. Rows
+  // that have seen nothing keep a reference of 0: no -inf - -inf.
+  if (__ballot(mx > s.m + 8.f)) {
+    const float mn = vmax(s.m, mx), alpha = __builtin_amdgcn_exp2f(s.m - (mn == -INFINITY ? 0.f : mn));
+    s.m = mn;
+    s.l *= alpha;
+#pragma unroll
+    for (int u = 0; u < HDP / 32; ++u) s.o[u] *= alpha;
+  }
+  const float ref = s.m == -INFINITY ? 0.f : s.m;
   float ps[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int st = 0; st < NS; ++st)
@@ -325,9 +441,7 @@ __device__ __forceinline__ void softmax_tile(Acc<HDP>& s, f32x16 (&sc)[NS], floa
       ps[i % 4] += p;
     }
   // (the sum takes the weights before their rounding to bf16: one rounding less)
-  s.l = s.l * alpha + ((ps[0] + ps[1]) + (ps[2] + ps[3]));
-#pragma unroll
-  for (int u = 0; u < HDP / 32; ++u) s.o[u] *= alpha;
+  s.l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
 }
 
 __device__ __forceinline__ bf16x8 weights_of(const f32x16& s, int c) {
@@ -423,61 +537,31 @@ __device__ __forceinline__ void put_stats(const PagedAttnArgs& a, const Item& it
   if (a.slots > 1) store_stats(a, row, 0, 0.f, -1.f);
 }
 
-// The lane's byte addresses for read_vt within a tile at LDS address `base`.
-template <int HDP>
-__device__ __forceinline__ void vt_addresses(unsigned base, unsigned (&ad)[4]) {
-  const int lane = threadIdx.x & 63, s = lane & 15, r = 4 * (lane >> 5) + (s >> 2);
-  const int c = 2 * ((lane >> 4) & 1) + ((s & 3) >> 1);
-  const unsigned a0 = r * Lay<HDP>::ROWB + ((c ^ Lay<HDP>::swz(r)) << 4) + ((s & 1) << 3);
-#pragma unroll
-  for (int u = 0; u < 4; ++u) ad[u] = base + (a0 ^ (u << 6));
-}
-
-// Fills the window of page offsets from entry e0 on; true where a page that
-// the item's keys need is not there.
-// (256 threads, all of them call it, and none reads the window or the flags
-// of an earlier call any more; ends with a barrier)
-struct Window { long off[PW]; int flag[4]; };
-
-__device__ __forceinline__ bool fill_window(const PagedAttnArgs& a, const Item& it, Window& win, int e0) {
-  const int n = (it.klim + (1 << a.kv.page_shift) - 1) >> a.kv.page_shift;
-  bool bad = false;
-#pragma unroll
-  for (int i = threadIdx.x; i < PW; i += 256) {
-    long off = -1;
-    if (e0 + i < n) {
-      off = page_offset(a, it.pages[e0 + i], it.g);
-      bad |= off < 0;
-      off = off < 0 ? -1 : off * 2;
-    }
-    win.off[i] = off;
-  }
-  const bool any = __ballot(bad) != 0;
-  if ((threadIdx.x & 63) == 0) win.flag[threadIdx.x >> 6] = any;
-  __syncthreads();
-  return (win.flag[0] | win.flag[1] | win.flag[2] | win.flag[3]) != 0;
-}
-
 // ---------------------------------------------------------------- bf16, waves split the rows
-// 128 rows a block, 32 a wave; the block's waves load each key tile together
-// into a ring of two. (K and V of 64 keys; 32 at head dim 256.)
-template <int HDP, bool CAP>
-__global__ void __launch_bounds__(256, 2) paged_rows_kernel(PagedAttnArgs a) {
+// 128 rows a block, 32 a wave; KS groups of four waves take every KS-th key
+// tile, whose four waves load it together, through a ring of two rounds. (64
+// keys a tile; 32 at head dim 256.) Two groups where the blocks are few: their
+// results meet in LDS.
+template <int HDP, bool CAP, int KS>
+__global__ void __launch_bounds__(256 * KS, 2) paged_rows_kernel(PagedAttnArgs a) {
   using Y = Lay<HDP>;
   constexpr int KT = HDP == 256 ? 32 : 64, NS = KT / 32, NC = HDP / 16, ND = HDP / 32;
-  constexpr int TILE = KT * Y::ROWB, IW = TILE / 4096;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * 2 * TILE];
+  constexpr int TILE = KT * Y::ROWB, ROUND = KS * 2 * TILE;
+  constexpr int MERGE = KS > 1 ? 256 * HDP * 2 : 0;       // half of each group's outputs
+  __shared__ __attribute__((aligned(1024))) char smem[2 * ROUND > MERGE ? 2 * ROUND : MERGE];
   __shared__ Window win;
+  __shared__ float stats[KS][128][2];
   Item it;
-  if (!find_item<128, KT, 1>(a, it)) return;
+  if (!find_item<128, KT, KS>(a, it)) return;
   const bool direct = a.direct && it.nranges <= 1;
   if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
     if (!direct) empty_range<128>(a, it);
     return;
   }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kg = wave >> 2, wr = wave & 3;
   const int lq = lane & 31, h = lane >> 5, hd = a.kv.hd, shift = a.kv.page_shift;
-  const int wrow = it.row0 + wave * 32;
+  const int wrow = it.row0 + wr * 32;
   const bool active = wrow < it.nrows;
   const Row w = row_of(a, it, wrow + lq);
   const WaveLimits wl = wave_limits<32>(a, w.lim);
@@ -498,71 +582,135 @@ __global__ void __launch_bounds__(256, 2) paged_rows_kernel(PagedAttnArgs a) {
 
   auto first_key = [&](int u) { return a.klo + (u < it.n1 ? u : u - it.n1 + it.t2) * KT; };
   const char *kb = reinterpret_cast<const char*>(a.kv.k), *vb = reinterpret_cast<const char*>(a.kv.v);
-  const char* Z = reinterpret_cast<const char*>(zero_piece);
-  const unsigned ts2 = (unsigned)(a.kv.tok_stride * 2), smask = (1u << shift) - 1;
+  const unsigned ring = lds_addr(smem);
   int w0 = 0;
   bool holes = false;
-  auto window = [&](int k0) {                  // (block-uniform; a barrier has passed since the last use)
-    const int e0 = k0 >> shift, e1 = max(k0, min(k0 + KT, it.klim) - 1) >> shift;
-    if (e0 >= w0 && e1 < w0 + PW) return;
-    w0 = e0;
-    holes |= fill_window(a, it, win, w0);
+  Mover<HDP, KT, 4> mv(a, win, wr);
+  auto issue = [&](int p) {                    // round p
+    const int u = it.ubeg + p * KS + kg;
+    if (u >= it.uend) return;
+    const unsigned dst = ring + (p & 1) * ROUND + kg * 2 * TILE;
+    mv.rows(first_key(u), w0, it.klim);
+    mv.template load<true>(kb, vb, dst, dst + TILE);
   };
-  auto issue = [&](int k0, unsigned dst) {
-#pragma unroll
-    for (int i = 0; i < IW; ++i) {
-      const int u = (i * 4 + wave) * 64 + lane, row = u / Y::CR, c = (u % Y::CR) ^ Y::swz(row), kk = k0 + row;
-      const long off = win.off[(min(kk, it.klim - 1) >> shift) - w0];
-      const long at = off + (unsigned long)(kk & smask) * ts2 + c * 16;
-      const bool ok = (kk < it.klim) & (c * 8 < hd) & (off >= 0);
-      const char *ks = ok ? kb + at : Z, *vs = ok ? vb + at : Z;
-      dma16(ks, dst + (i * 4 + wave) * 1024);
-      dma16(vs, dst + TILE + (i * 4 + wave) * 1024);
-    }
-  };
-  if (it.ubeg < it.uend) {
+  const int nrounds = (it.uend - it.ubeg + KS - 1) / KS;
+  if (nrounds > 0) {
     w0 = first_key(it.ubeg) >> shift;
-    holes = fill_window(a, it, win, w0);
-    issue(first_key(it.ubeg), lds_addr(smem));
+    holes = fill_window<256 * KS>(a, it, win, w0);
+    issue(0);
   }
   hold(qf);
-  for (int u = it.ubeg; u < it.uend; ++u) {
-    // this tile has landed, and every wave is done with the tile before
+  // where the lane's K and V fragments begin; the swizzled pieces of a row
+  // differ in address bits only, which costs an instruction a read and no
+  // registers (held for all pieces they spill at head dim 256)
+  const unsigned ka = lq * Y::ROWB + ((h ^ Y::swz(lq)) << 4), va = vt_address<HDP>();
+  for (int p = 0; p < nrounds; ++p) {
+    // this round has landed, and every wave is done with the round before
     asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    char* Kt = smem + ((u - it.ubeg) & 1) * 2 * TILE;
-    const int k0 = first_key(u);
-    if (u + 1 < it.uend) {
-      window(first_key(u + 1));
-      issue(first_key(u + 1), lds_addr(smem) + ((u + 1 - it.ubeg) & 1) * 2 * TILE);
+    if (p + 1 < nrounds) {
+      const int n0 = first_key(it.ubeg + (p + 1) * KS), e0 = n0 >> shift, e1 = (min(n0 + KS * KT, it.klim) - 1) >> shift;
+      if (e0 < w0 || e1 >= w0 + PW) {          // (block-uniform; the barrier was the window's last use)
+        w0 = e0;
+        holes |= fill_window<256 * KS>(a, it, win, w0);
+      }
+      issue(p + 1);
     }
-    if (!active || tile_unseen(wl, k0, k0 + KT)) continue;
+    const int u = it.ubeg + p * KS + kg, k0 = first_key(u);
+    if (!active || u >= it.uend || tile_unseen(wl, k0, k0 + KT)) continue;
+    unsigned kt = ring + (p & 1) * ROUND + kg * 2 * TILE + ka, vt = kt - ka + TILE + va;
+    asm volatile("" : "+v"(kt), "+v"(vt));
+    // fragments are requested well ahead of their products (LDS answers after
+    // a few of these): all keys' first, two groups of the values' before the
+    // softmax (head dim 256 has no registers for that)
     f32x16 sc[NS];
+    bf16x8 kf[HDP <= 128 ? NS : 1][NC];
+    constexpr bool AHEAD = HDP <= 128;
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int st = 0; st < NS; ++st)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) kf[st][c] = read_k(kt, c, st * 32 * Y::ROWB);
+      __builtin_amdgcn_sched_barrier(0);
+    }
 #pragma unroll
     for (int st = 0; st < NS; ++st) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[st][i] = 0.f;
-      const int row = st * 32 + lq;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(Kt + row * Y::ROWB + (((2 * c + h) ^ Y::swz(row)) << 4));
-        sc[st] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[c], sc[st], 0, 0, 0);
+        if constexpr (!AHEAD) kf[0][c] = read_k(kt, c, st * 32 * Y::ROWB);
+        sc[st] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[AHEAD ? st : 0][c], qf[c], sc[st], 0, 0, 0);
       }
     }
+    bf16x8 vf[2][ND];
+    auto values = [&](int c) {
+#pragma unroll
+      for (int u2 = 0; u2 < ND; ++u2) vf[c % 2][u2] = read_vt<HDP>(vt, u2, c * 16 * Y::ROWB);
+    };
+    if constexpr (AHEAD) {
+      values(0);
+      values(1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     softmax_tile<HDP, NS, CAP>(s, sc, sl2, c1, c2, !holes && tile_full(wl, k0, k0 + KT), w.lim, k0, a, it, holes);
-    unsigned ad[4];
-    vt_addresses<HDP>(lds_addr(Kt + TILE), ad);
 #pragma unroll
     for (int c = 0; c < KT / 16; ++c) {
-      const bf16x8 p = weights_of(sc[c / 2], c % 2);
+      const bf16x8 pf = weights_of(sc[c / 2], c % 2);
+      if constexpr (!AHEAD) values(c);
 #pragma unroll
       for (int u2 = 0; u2 < ND; ++u2)
-        s.o[u2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_vt<HDP>(ad, u2, c * 16 * Y::ROWB), p, s.o[u2], 0, 0, 0);
+        s.o[u2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c % 2][u2], pf, s.o[u2], 0, 0, 0);
+      if constexpr (AHEAD)
+        if (c + 2 < KT / 16) values(c + 2);
     }
   }
-  if (!active) return;
   s.l = sum_x32(s.l);
-  repair<HDP, CAP>(a, it, s, qf, w.lim, sl2, c1, c2, max(0, it.uend - it.ubeg), KT,
-                   [&](int n) { return first_key(it.ubeg + n); });
+  if (active) {
+    const int mine = it.uend - it.ubeg - kg;
+    repair<HDP, CAP>(a, it, s, qf, w.lim, sl2, c1, c2, mine > 0 ? (mine + KS - 1) / KS : 0, KT,
+                     [&](int n) { return first_key(it.ubeg + n * KS + kg); });
+  }
+  if constexpr (KS == 2) {
+    // each group keeps half of the dims and hands the other half over
+    __syncthreads();                           // the ring is free
+    f32x4* mo = reinterpret_cast<f32x4*>(smem);
+    auto slot = [&](int g, int j) { return ((g * 4 + wr) * (ND * 2) + j) * 64 + lane; };
+    if (h == 0) {
+      stats[kg][wr * 32 + lq][0] = s.m;
+      stats[kg][wr * 32 + lq][1] = s.l;
+    }
+    auto hand = [&](auto from) {
+      constexpr int U = decltype(from)::value;
+#pragma unroll
+      for (int j = 0; j < ND * 2; ++j) {
+        const f32x16& x = s.o[U + j / 4];
+        mo[slot(kg, j)] = f32x4{x[4 * (j % 4)], x[4 * (j % 4) + 1], x[4 * (j % 4) + 2], x[4 * (j % 4) + 3]};
+      }
+    };
+    if (kg == 0) hand(std::integral_constant<int, ND / 2>{});
+    else hand(std::integral_constant<int, 0>{});
+    __syncthreads();
+    if (wrow + lq >= it.nrows) return;
+    const float m2 = stats[1 - kg][wr * 32 + lq][0], l2 = stats[1 - kg][wr * 32 + lq][1], m = vmax(s.m, m2);
+    // (a group without keys weighs nothing)
+    const float w1 = s.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.m - m);
+    const float w2 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m2 - m);
+    const float l = kg == 0 ? s.l * w1 + l2 * w2 : l2 * w2 + s.l * w1, inv = inverse(l);
+    auto finish = [&](auto from) {
+      constexpr int U = decltype(from)::value;
+#pragma unroll
+      for (int j = 0; j < ND * 2; ++j) {
+        const f32x16& x = s.o[U + j / 4];
+        const f32x4 mine = f32x4{x[4 * (j % 4)], x[4 * (j % 4) + 1], x[4 * (j % 4) + 2], x[4 * (j % 4) + 3]} * w1;
+        const f32x4 y = w2 == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : mo[slot(1 - kg, j)] * w2;
+        put(a, it, w, direct, 32 * (U + j / 4) + 8 * (j % 4) + 4 * h, mine + y, inv);
+      }
+    };
+    if (kg == 0) finish(std::integral_constant<int, 0>{});
+    else finish(std::integral_constant<int, ND / 2>{});
+    if (kg == 0 && h == 0) put_stats(a, it, w, direct, m, l);
+    return;
+  }
   if (wrow + lq >= it.nrows) return;
   const float inv = inverse(s.l);
 #pragma unroll
@@ -614,33 +762,21 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
   const float sl2 = a.scale * LOG2E, c1 = CAP ? 2.f * sl2 / a.cap : 0.f, c2 = a.cap * LOG2E;
   auto first_key = [&](int u) { return a.klo + (u < it.n1 ? u : u - it.n1 + it.t2) * KT; };
   const char *kb = reinterpret_cast<const char*>(a.kv.k), *vb = reinterpret_cast<const char*>(a.kv.v);
-  const char* Z = reinterpret_cast<const char*>(zero_piece);
-  const unsigned ts2 = (unsigned)(a.kv.tok_stride * 2), smask = (1u << shift) - 1;
   int w0 = 0;
   bool holes = false;
   char *slot_k = smem + wave * 2 * TILE, *slot_v = slot_k + TILE;
-  auto issue = [&](int k0, const char* base, unsigned dst) {
-#pragma unroll
-    for (int i = 0; i < LK; ++i) {
-      const int u = i * 64 + lane, row = u / Y::CR, c = (u % Y::CR) ^ Y::swz(row), kk = k0 + row;
-      // (keys behind the last read the entry of the last, or the window's first)
-      const long off = win.off[max(0, (min(kk, it.klim - 1) >> shift) - w0)];
-      const bool ok = (kk < it.klim) & (c * 8 < hd) & (off >= 0);
-      const char* p = ok ? base + (off + (unsigned long)(kk & smask) * ts2 + c * 16) : Z;
-      dma16(p, dst + i * 1024);
-    }
-  };
+  Mover<HDP, KT, 1> mv(a, win, 0);
   const int nrounds = (it.uend - it.ubeg + NW - 1) / NW;
   if (nrounds > 0) {
     w0 = first_key(it.ubeg) >> shift;
-    holes = fill_window(a, it, win, w0);
+    holes = fill_window<256>(a, it, win, w0);
     if (it.ubeg + wave < it.uend) {
-      issue(first_key(it.ubeg + wave), kb, lds_addr(slot_k));
-      issue(first_key(it.ubeg + wave), vb, lds_addr(slot_v));
+      mv.rows(first_key(it.ubeg + wave), w0, it.klim);
+      mv.template load<false>(kb, nullptr, lds_addr(slot_k), 0);
+      mv.template load<false>(vb, nullptr, lds_addr(slot_v), 0);
     }
   }
-  unsigned ad[4];
-  vt_addresses<HDP>(lds_addr(slot_v), ad);
+  const unsigned va = lds_addr(slot_v) + vt_address<HDP>(), ka = lds_addr(slot_k) + lq * Y::ROWB + ((h ^ Y::swz(lq)) << 4);
   hold(qf);
 #pragma unroll 1
   for (int p = 0; p < nrounds; ++p) {
@@ -652,7 +788,7 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
       if (e0 < w0 || e1 >= w0 + PW) {
         __syncthreads();
         w0 = e0;
-        holes |= fill_window(a, it, win, w0);
+        holes |= fill_window<256>(a, it, win, w0);
       }
     }
     if (u >= it.uend) continue;
@@ -661,10 +797,13 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
     bf16x8 kf[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c)
-      kf[c] = *reinterpret_cast<const bf16x8*>(slot_k + lq * Y::ROWB + (((2 * c + h) ^ Y::swz(lq)) << 4));
+      kf[c] = read_k(ka, c, 0);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    if (next) issue(first_key(u + NW), kb, lds_addr(slot_k));
+    if (next) {
+      mv.rows(first_key(u + NW), w0, it.klim);
+      mv.template load<false>(kb, nullptr, lds_addr(slot_k), 0);
+    }
     f32x16 sc[1];
 #pragma unroll
     for (int i = 0; i < 16; ++i) sc[0][i] = 0.f;
@@ -678,10 +817,10 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
-      for (int u2 = 0; u2 < ND; ++u2) vf[c][u2] = read_vt<HDP>(ad, u2, c * 16 * Y::ROWB);
+      for (int u2 = 0; u2 < ND; ++u2) vf[c][u2] = read_vt<HDP>(va, u2, c * 16 * Y::ROWB);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    if (next) issue(first_key(u + NW), vb, lds_addr(slot_v));
+    if (next) mv.template load<false>(vb, nullptr, lds_addr(slot_v), 0);
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const bf16x8 pf = weights_of(sc[0], c);
@@ -914,79 +1053,128 @@ __global__ void __launch_bounds__(512) paged_f32_kernel(PagedAttnArgs a) {
 }
 
 // ---------------------------------------------------------------- merge of ranges
-// One block a row: its four waves take every fourth slot, their sums meet in
-// LDS in wave order. A lane owns four dims.
-template <typename T>
+// LPR lanes own a row, four dims each, and WPR such groups share its slots,
+// eight at a time (their statistics and outputs in one round trip), merged in
+// order; the groups' sums meet in LDS in group order.
+template <typename T, int LPR, int WPR>
 __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a) {
-  __shared__ float st[4][2];
-  __shared__ __attribute__((aligned(16))) f32x4 acc[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, S = a.slots, hd = a.kv.hd;
-  const int tok = blockIdx.x, head = blockIdx.y;
-  const long row = (long)tok * a.n_q + head;
-  if (tok < a.bt.start[0] || tok >= a.bt.start[a.bt.n_req]) return;
+  constexpr int RB = 256 / (LPR * WPR), N = 8;
+  const int tid = threadIdx.x, sub = tid % LPR, grp = tid / LPR % WPR, S = a.slots, hd = a.kv.hd;
+  const long row = blockIdx.x * (long)RB + tid / (LPR * WPR);
+  const int tok = (int)(row / a.n_q), head = (int)(row - (long)tok * a.n_q);
   const float* stat = a.ws + (long)a.bt.n_tok * a.n_q * S * hd + row * S * 2;
-  if (stat[1] < 0.f) return;                   // written already
-  float m = -INFINITY;
-  for (int i = lane; i < S; i += 64) m = vmax(m, stat[2 * i + 1] == 0.f ? -INFINITY : stat[2 * i]);
-  for (int o = 32; o > 0; o >>= 1) m = vmax(m, __shfl_xor(m, o));
+  // rows of no request, and those that are written already
+  bool live = tok < a.bt.n_tok && tok >= a.bt.start[0] && tok < a.bt.start[a.bt.n_req];
+  live = live && !(stat[1] < 0.f);
+  const bool dok = sub * 4 < hd;
+  float m = -INFINITY, l = 0.f;
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
-#pragma unroll 4
-  for (int i = wave; i < S; i += 4) {
-    const float ms = stat[2 * i], ls = stat[2 * i + 1];
-    if (ls == 0.f) continue;                   // (no keys; a NaN sum is not 0)
-    const float w = __builtin_amdgcn_exp2f(ms - m);
-    l += ls * w;
-    if (lane * 4 < hd) s += *reinterpret_cast<const f32x4*>(part_of(a, row, i) + lane * 4) * w;
+  for (int b = grp * N; live && b < S; b += WPR * N) {
+    float ms[N], ls[N];
+    f32x4 pt[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const bool in = b + k < S;
+      ms[k] = in ? stat[2 * (b + k)] : 0.f;
+      ls[k] = in ? stat[2 * (b + k) + 1] : 0.f;
+      pt[k] = in && dok ? *reinterpret_cast<const f32x4*>(part_of(a, row, b + k) + sub * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // (a range without keys has a sum of 0 and no output; a NaN sum is not 0)
+    float mb = m;
+#pragma unroll
+    for (int k = 0; k < N; ++k) mb = ls[k] == 0.f ? mb : vmax(mb, ms[k]);
+    const float w0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mb);
+    l *= w0;
+    s *= w0;
+    m = mb;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float w = __builtin_amdgcn_exp2f(ms[k] - mb);
+      if (ls[k] == 0.f) continue;
+      l += ls[k] * w;
+      s += pt[k] * w;
+    }
   }
-  if (lane == 0) st[wave][0] = l;
-  acc[wave][lane] = s;
-  __syncthreads();
-  if (wave != 0) return;
-  l = (st[0][0] + st[1][0]) + (st[2][0] + st[3][0]);
-  s = (acc[0][lane] + acc[1][lane]) + (acc[2][lane] + acc[3][lane]);
+  if constexpr (WPR > 1) {
+    __shared__ float st[256][2];
+    __shared__ __attribute__((aligned(16))) f32x4 acc[256];
+    st[tid][0] = m;
+    st[tid][1] = l;
+    acc[tid] = s;
+    __syncthreads();
+    if (grp != 0) return;
+    float mm = m;
+#pragma unroll
+    for (int g = 1; g < WPR; ++g) mm = vmax(mm, st[tid + g * LPR][0]);
+    const float w0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mm);
+    l *= w0;
+    s *= w0;
+#pragma unroll
+    for (int g = 1; g < WPR; ++g) {
+      const float mg = st[tid + g * LPR][0];
+      if (mg == -INFINITY) continue;
+      const float w = __builtin_amdgcn_exp2f(mg - mm);
+      l += st[tid + g * LPR][1] * w;
+      s += acc[tid + g * LPR] * w;
+    }
+    m = mm;
+  }
+  if (!live) return;
   const float inv = inverse(l);
-  if (lane * 4 < hd) {
-    T* op = reinterpret_cast<T*>(a.o) + (long)tok * a.o_ts + (long)head * a.o_hs + lane * 4;
+  if (dok) {
+    T* op = reinterpret_cast<T*>(a.o) + (long)tok * a.o_ts + (long)head * a.o_hs + sub * 4;
     if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x4*>(op) = bf16x4{(bf16)(s[0] * inv), (bf16)(s[1] * inv), (bf16)(s[2] * inv), (bf16)(s[3] * inv)};
     else *reinterpret_cast<f32x4*>(op) = s * inv;
   }
-  if (a.lse && lane == 0) a.lse[row] = m * LN2 + logf(l);
+  if (a.lse && sub == 0) a.lse[row] = m * LN2 + logf(l);
 }
 
 }  // namespace
 
 // ---------------------------------------------------------------- host
-// Rows of a tile and keys of a key tile of kernel k at padded head dim hdp.
-static int tile_rows(int k) { return k == 0 ? 32 : k == 1 ? 128 : 16; }
-static int tile_keys(int k, int hdp) { return k == 0 ? 32 : k == 1 ? (hdp == 256 ? 32 : 64) : 16; }
+// Rows of a tile, keys of a key tile and key tiles of a round of kernel k at
+// padded head dim hdp.
+static int tile_rows(int k) { return k == PAGED_KEYS ? 32 : k == PAGED_F32 ? 16 : 128; }
+static int tile_keys(int k, int hdp) { return k == PAGED_KEYS ? 32 : k == PAGED_F32 ? 16 : hdp == 256 ? 32 : 64; }
+static int round_tiles(int k) { return k == PAGED_KEYS ? 4 : k == PAGED_ROWS2 ? 2 : 1; }
 
-// Key ranges of a part: enough blocks for two a CU, ranges of 2048 keys at
-// most for single tokens (requests differ in length: short ranges share the
-// work evenly), of 256 at least.
-static void cut(PagedPart& p, int hdp, int keys, int n_kv) {
-  const int kt = tile_keys(p.kernel, hdp), unit = p.kernel == 0 ? 4 : 1;   // (lists are padded to whole units)
-  auto up = [](long x, long m) { return (x + m - 1) / m * m; };
-  const long total = up(std::max(1, (keys + kt - 1) / kt), unit), blocks = (long)p.tiles * n_kv;
-  long want = (512 + blocks - 1) / blocks;
-  if (p.kernel == 0) want = std::max<long>(want, (keys + 2047) / 2048);
-  long per = up(std::max<long>(256 / kt, (total + want - 1) / want), unit);
-  per = std::max(per, up((total + 65534) / 65535, unit));                  // (the grid's second extent)
-  p.chunk = (int)per;
-  p.ranges = (int)((total + per - 1) / per);
+// Key ranges of a part: the count that minimises the time of a simple model:
+// waves of resident blocks times (start + rounds of tiles), and where a row has
+// several ranges the merge's launch and the bytes of the outputs it reads.
+static void cut(PagedPart& p, int hdp, int hd, int keys, int n_kv, long rows) {
+  const int kt = tile_keys(p.kernel, hdp), unit = round_tiles(p.kernel);
+  const long total = std::max(1, (keys + kt * unit - 1) / (kt * unit));      // rounds
+  const long blocks = (long)p.tiles * n_kv;
+  const long resident = p.kernel == PAGED_ROWS2 || hdp == 256 ? 256 : 512;
+  const double start = 3.0, merge = 3.0, bytes = 4.0 * kt * unit * hd;
+  double best = 1e30;
+  long best_per = total;
+  const long most = p.kernel == PAGED_KEYS || p.kernel == PAGED_F32 ? 256 : std::max<long>(1, resident / blocks);
+  for (long s = 1; s <= std::min(total, most); ++s) {
+    const long per = (total + s - 1) / s, n = (total + per - 1) / per;
+    if (n != s) continue;
+    const double on = (double)std::min(blocks * s, resident);
+    const double round = std::max(1.0, bytes * on / 5e6);                     // us
+    const double t = (double)((blocks * s + resident - 1) / resident) * (start + per * round) +
+                     (s > 1 ? merge + rows * (double)s * hd * 8 / 4e6 : 0.0);
+    if (t < best) { best = t; best_per = per; }
+  }
+  best_per = std::max<long>(best_per, (total + 65534) / 65535);               // (the grid's second extent)
+  p.chunk = (int)(best_per * unit);
+  p.ranges = (int)((total + best_per - 1) / best_per);
 }
 
 PagedPlan paged_plan(const PagedAttnArgs& a, int et) {
   PagedPlan p{};
   p.hdp = a.kv.hd <= 64 ? 64 : a.kv.hd <= 128 ? 128 : 256;
+  const long all = (long)a.bt.n_tok * a.G;
   auto part = [&](long rows_req, bool flat, int keys) {
     PagedPart q{};
-    const long rows = flat ? (long)a.bt.n_tok * a.G : rows_req;
-    q.kernel = et == ET_F32 ? 2 : rows <= 32 ? 0 : 1;
+    q.kernel = et == ET_F32 ? PAGED_F32 : (flat ? all : rows_req) <= 32 ? PAGED_KEYS : PAGED_ROWS;
     const int br = tile_rows(q.kernel);
-    const long all = (long)a.bt.n_tok * a.G;
     q.tiles = (int)(flat ? std::max<long>(1, (all + br - 1) / br) : rows_req <= br ? a.bt.n_req : all / br + a.bt.n_req);
-    cut(q, p.hdp, keys, a.kv.n_kv);
+    if (q.kernel == PAGED_ROWS && (long)q.tiles * a.kv.n_kv <= 256) q.kernel = PAGED_ROWS2;
+    cut(q, p.hdp, a.kv.hd, keys, a.kv.n_kv, (long)a.bt.n_tok * a.n_q);
     return q;
   };
   const long rows_req = (long)a.bt.max_new * a.G;
@@ -1011,9 +1199,24 @@ size_t paged_attention_ws(const PagedAttnArgs& a, int et) {
 template <int HDP, bool CAP>
 static void launch_part(const PagedAttnArgs& a, int kernel, hipStream_t s) {
   const dim3 grid((unsigned)a.tiles * a.kv.n_kv, a.ranges);
-  if (kernel == 0) hipLaunchKernelGGL((paged_keys_kernel<HDP, CAP>), grid, dim3(256), 0, s, a);
-  else if (kernel == 1) hipLaunchKernelGGL((paged_rows_kernel<HDP, CAP>), grid, dim3(256), 0, s, a);
+  if (kernel == PAGED_KEYS) hipLaunchKernelGGL((paged_keys_kernel<HDP, CAP>), grid, dim3(256), 0, s, a);
+  else if (kernel == PAGED_ROWS) hipLaunchKernelGGL((paged_rows_kernel<HDP, CAP, 1>), grid, dim3(256), 0, s, a);
+  else if (kernel == PAGED_ROWS2) hipLaunchKernelGGL((paged_rows_kernel<HDP, CAP, 2>), grid, dim3(512), 0, s, a);
   else hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP>), grid, dim3(512), 0, s, a);
+}
+
+template <typename T, int LPR>
+static void launch_merge(const PagedAttnArgs& a, long rows, hipStream_t s) {
+  const int wpr = a.slots > 8 ? 4 : 1, rb = 256 / (LPR * wpr);
+  const dim3 grid((unsigned)((rows + rb - 1) / rb));
+  if (wpr == 4) hipLaunchKernelGGL((paged_merge_kernel<T, LPR, 4>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged_merge_kernel<T, LPR, 1>), grid, dim3(256), 0, s, a);
+}
+template <typename T>
+static void launch_merge(const PagedAttnArgs& a, int hdp, long rows, hipStream_t s) {
+  if (hdp == 64) launch_merge<T, 16>(a, rows, s);
+  else if (hdp == 128) launch_merge<T, 32>(a, rows, s);
+  else launch_merge<T, 64>(a, rows, s);
 }
 
 void launch_paged_attention(const PagedAttnArgs& a, int et, hipStream_t s) {
@@ -1038,8 +1241,8 @@ void launch_paged_attention(const PagedAttnArgs& a, int et, hipStream_t s) {
   if (p.slots > 1) {
     PagedAttnArgs b = a;
     b.slots = p.slots;
-    const dim3 grid(a.bt.n_tok, a.n_q);
-    if (et == ET_BF16) hipLaunchKernelGGL(paged_merge_kernel<bf16>, grid, dim3(256), 0, s, b);
-    else hipLaunchKernelGGL(paged_merge_kernel<float>, grid, dim3(256), 0, s, b);
+    const long rows = (long)a.bt.n_tok * a.n_q;
+    if (et == ET_BF16) launch_merge<bf16>(b, p.hdp, rows, s);
+    else launch_merge<float>(b, p.hdp, rows, s);
   }
 }

@@ -61,7 +61,7 @@ void fill(const vla_kv_pool* p, const vla_ragged* b, bool buffers, PagedKV& kv, 
   check_stride(p->page_stride, p->n_pages, p->head_dim, es, "pool page");
   check_stride(p->head_stride, p->n_kv, p->head_dim, es, "pool head");
   check_stride(p->token_stride, p->page_tokens, p->head_dim, es, "pool token");
-  VLA_REQUIRE(p->page_tokens == 1 || p->token_stride * es < (1LL << 31), "pool token stride must be below 2^31 bytes");
+  VLA_REQUIRE(p->page_tokens == 1 || p->token_stride * es < (1LL << 28), "pool token stride must be below 2^28 bytes");
   if (buffers) {
     VLA_REQUIRE(p->k && p->v && aligned(p->k, 16) && aligned(p->v, 16), "pool k and v must be 16-byte aligned buffers");
     VLA_REQUIRE(b->start && b->kv_len && (b->pages || b->pages_stride == 0), "null start, kv_len or pages");
