@@ -283,24 +283,25 @@ __device__ __forceinline__ bf16x8 read_k(unsigned at, int c, int off) {
 
 // The window of page offsets a block keeps in LDS (bytes from the pool's bases
 // of this KV head's rows; -1: not there), entries w0 .. w0 + PW - 1.
-constexpr int PW = 512;
+constexpr int PW = 256;
 
 // Fills the window of page offsets from entry e0 on; true where a page that
 // the item's keys need is not there.
-// (all threads of the block call it, and none reads the window or the flags
-// of an earlier call any more; ends with a barrier)
+// (all threads of the block, at least PW, call it, and none reads the window or the flags
+// of an earlier call any more; ends with a barrier; `guessed`: this
+// thread's entry of the window from entry `guess` on, requested earlier)
 struct Window { long off[PW]; int flag[8]; };
 
 template <int THREADS>
-__device__ __forceinline__ bool fill_window(const PagedAttnArgs& a, const Item& it, Window& win, int e0) {
-  const int n = (it.klim + (1 << a.kv.page_shift) - 1) >> a.kv.page_shift;
+__device__ __forceinline__ bool fill_window(const PagedAttnArgs& a, const Item& it, Window& win, int e0, int guess = -1,
+                                            int guessed = 0) {
+  const int n = (it.klim + (1 << a.kv.page_shift) - 1) >> a.kv.page_shift, i = threadIdx.x;
   bool bad = false;
-#pragma unroll
-  for (int i = threadIdx.x; i < PW; i += THREADS) {
+  if (THREADS == PW || i < PW) {
     long off = -1;
     if (e0 + i < n) {
-      off = page_offset(a, it.pages[e0 + i], it.g);
-      bad |= off < 0;
+      off = page_offset(a, e0 == guess ? guessed : it.pages[e0 + i], it.g);
+      bad = off < 0;
       off = off < 0 ? -1 : off * 2;
     }
     win.off[i] = off;
@@ -310,7 +311,7 @@ __device__ __forceinline__ bool fill_window(const PagedAttnArgs& a, const Item& 
   __syncthreads();
   int f = 0;
 #pragma unroll
-  for (int i = 0; i < THREADS / 64; ++i) f |= win.flag[i];
+  for (int w = 0; w < PW / 64; ++w) f |= win.flag[w];
   return f != 0;
 }
 
@@ -722,62 +723,91 @@ __global__ void __launch_bounds__(256 * KS, 2) paged_rows_kernel(PagedAttnArgs a
 }
 
 // ---------------------------------------------------------------- bf16, waves split the keys
-// 32 rows a block; wave w takes every fourth tile of 32 keys into a K and a V
-// slot of its own and waits for its own loads only: no barrier in the loop, and
-// a slot is loaded again as soon as its fragments are in registers. The waves'
-// (max, sum, output) meet in LDS at the end. For single tokens, whose time is
-// that of the keys' and values' bytes.
-template <int HDP, bool CAP>
+// 16 RT rows a block; wave w takes every fourth tile of 32 keys into a K and a
+// V slot of its own and waits for its own loads only: no barrier in the loop,
+// and a slot is loaded again as soon as its fragments are in registers. The
+// waves' (max, sum, output) meet in LDS at the end. For single tokens, whose
+// time is that of the keys' and values' bytes, or where those are few, of the
+// chain of memory round trips and of the instructions (cold in each launch):
+// hence 16-row products (v_mfma_f32_16x16x32), which for the usual few query
+// heads a KV head leave half the registers and code of the 32-row ones.
+// Lane l holds of S^T the keys 16 st + 4 (l / 16) + 0..3 of row l % 16, which
+// is key slot order 4 (l / 16) + 0..3, 16 + 4 (l / 16) + 0..3 of the second product.
+__device__ __forceinline__ float max_x16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return vmax(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_x16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+template <int HDP, int RT, bool CAP>
 __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(PagedAttnArgs a) {
   using Y = Lay<HDP>;
-  constexpr int KT = 32, NW = 4, NC = HDP / 16, ND = HDP / 32, TILE = KT * Y::ROWB, LK = TILE / 1024;
-  __shared__ __attribute__((aligned(1024))) char smem[NW * 2 * TILE];
+  constexpr int KT = 32, NW = 4, NC = HDP / 32, ND = HDP / 16, TILE = KT * Y::ROWB, LK = TILE / 1024;
+  constexpr int MERGE = NW * RT * ND * 1024;
+  __shared__ __attribute__((aligned(1024))) char smem[NW * 2 * TILE > MERGE ? NW * 2 * TILE : MERGE];
   __shared__ Window win;
-  __shared__ float stats[NW][32][2];
-  static_assert(NW * 2 * TILE == NW * 64 * ND * 64, "the waves' outputs fill the slots");
+  __shared__ float stats[NW][16 * RT][2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), shift = a.kv.page_shift;
+  // the page numbers that the range needs if no window moves it: requested with the batch's lengths
+  const int guess = (a.klo + (int)blockIdx.y * a.chunk * KT) >> shift;
+  int guessed = 0;
+  if (a.bt.pages_stride > 0) {
+    const int tile = (int)blockIdx.x / a.kv.n_kv, r = a.flat ? 0 : (a.causal ? a.tiles - 1 - tile : tile);
+    guessed = a.bt.pages[(long)r * a.bt.pages_stride + min(guess + tid, a.bt.pages_stride - 1)];
+  }
   Item it;
-  if (!find_item<32, KT, NW>(a, it)) return;
+  if (!find_item<16 * RT, KT, NW>(a, it)) return;
   const bool direct = a.direct && it.nranges <= 1;
   if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
-    if (!direct) empty_range<32>(a, it);
+    if (!direct) empty_range<16 * RT>(a, it);
     return;
   }
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lq = lane & 31, h = lane >> 5, hd = a.kv.hd, shift = a.kv.page_shift;
-  const Row w = row_of(a, it, it.row0 + lq);
-  const WaveLimits wl = wave_limits<32>(a, w.lim);
-  bf16x8 qf[NC];
-  {
-    const bf16* qp = reinterpret_cast<const bf16*>(a.q) + (long)w.tok * a.q_ts + (long)w.head * a.q_hs;
+  const int lq = lane & 15, grp = lane >> 4, hd = a.kv.hd;
+  Row w[RT];
+  WaveLimits wl;
+  bf16x8 qf[RT][NC];
+  f32x4 o[RT][ND];
+  float m[RT], l[RT];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) qf[c] = 16 * c + 8 * h < hd ? *reinterpret_cast<const bf16x8*>(qp + 16 * c + 8 * h) : bf16x8{};
+  for (int t = 0; t < RT; ++t) {
+    w[t] = row_of(a, it, it.row0 + t * 16 + lq);
+    const WaveLimits x = wave_limits<16>(a, w[t].lim);
+    wl = t == 0 ? x : WaveLimits{min(wl.pre0, x.pre0), max(wl.pre1, x.pre1), min(wl.lo0, x.lo0), max(wl.lo1, x.lo1),
+                                 min(wl.hi0, x.hi0), max(wl.hi1, x.hi1)};
+    const bf16* qp = reinterpret_cast<const bf16*>(a.q) + (long)w[t].tok * a.q_ts + (long)w[t].head * a.q_hs;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      qf[t][c] = 32 * c + 8 * grp < hd ? *reinterpret_cast<const bf16x8*>(qp + 32 * c + 8 * grp) : bf16x8{};
+#pragma unroll
+    for (int u = 0; u < ND; ++u) o[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m[t] = -INFINITY;
+    l[t] = 0.f;
   }
-  Acc<HDP> s;
-#pragma unroll
-  for (int u = 0; u < ND; ++u)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s.o[u][i] = 0.f;
-  s.m = -INFINITY;
-  s.l = 0.f;
   const float sl2 = a.scale * LOG2E, c1 = CAP ? 2.f * sl2 / a.cap : 0.f, c2 = a.cap * LOG2E;
   auto first_key = [&](int u) { return a.klo + (u < it.n1 ? u : u - it.n1 + it.t2) * KT; };
   const char *kb = reinterpret_cast<const char*>(a.kv.k), *vb = reinterpret_cast<const char*>(a.kv.v);
   int w0 = 0;
   bool holes = false;
-  char *slot_k = smem + wave * 2 * TILE, *slot_v = slot_k + TILE;
+  const unsigned slot_k = lds_addr(smem) + wave * 2 * TILE, slot_v = slot_k + TILE;
   Mover<HDP, KT, 1> mv(a, win, 0);
   const int nrounds = (it.uend - it.ubeg + NW - 1) / NW;
   if (nrounds > 0) {
     w0 = first_key(it.ubeg) >> shift;
-    holes = fill_window<256>(a, it, win, w0);
+    holes = fill_window<256>(a, it, win, w0, guess, guessed);
     if (it.ubeg + wave < it.uend) {
       mv.rows(first_key(it.ubeg + wave), w0, it.klim);
-      mv.template load<false>(kb, nullptr, lds_addr(slot_k), 0);
-      mv.template load<false>(vb, nullptr, lds_addr(slot_v), 0);
+      mv.template load<false>(kb, nullptr, slot_k, 0);
+      mv.template load<false>(vb, nullptr, slot_v, 0);
     }
   }
-  const unsigned va = lds_addr(slot_v) + vt_address<HDP>(), ka = lds_addr(slot_k) + lq * Y::ROWB + ((h ^ Y::swz(lq)) << 4);
-  hold(qf);
+#pragma unroll
+  for (int t = 0; t < RT; ++t) hold(qf[t]);
+  const unsigned ka = slot_k + lq * Y::ROWB + ((grp ^ Y::swz(lq)) << 4);
+  const int vr = 4 * grp + (lq >> 2);
+  const unsigned va = slot_v + vr * Y::ROWB + ((((lq & 3) >> 1) ^ Y::swz(vr)) << 4) + ((lq & 1) << 3);
 #pragma unroll 1
   for (int p = 0; p < nrounds; ++p) {
     const int u = it.ubeg + p * NW + wave, k0 = first_key(u);
@@ -794,82 +824,169 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
     if (u >= it.uend) continue;
     // this tile's keys have landed once only its values' loads are pending
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LK) : "memory");
-    bf16x8 kf[NC];
+    bf16x8 kf[2][NC];
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-      kf[c] = read_k(ka, c, 0);
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        typedef const __attribute__((address_space(3))) bf16x8* P;
+        kf[st][c] = *(P)(uintptr_t)((ka ^ (c % 4 << 6)) + st * 16 * Y::ROWB + c / 4 * 256);
+      }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     if (next) {
       mv.rows(first_key(u + NW), w0, it.klim);
-      mv.template load<false>(kb, nullptr, lds_addr(slot_k), 0);
+      mv.template load<false>(kb, nullptr, slot_k, 0);
     }
-    f32x16 sc[1];
+    const bool full = !holes && tile_full(wl, k0, k0 + KT);
+    bf16x8 pf[RT];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sc[0][i] = 0.f;
+    for (int t = 0; t < RT; ++t) {
+      f32x4 sc[2];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], qf[c], sc[0], 0, 0, 0);
-    softmax_tile<HDP, 1, CAP>(s, sc, sl2, c1, c2, !holes && tile_full(wl, k0, k0 + KT), w.lim, k0, a, it, holes);
+      for (int st = 0; st < 2; ++st) {
+        f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;         // two chains
+#pragma unroll
+        for (int c = 0; c < NC; c += 2) {
+          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[st][c], qf[t][c], s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[st][c + 1], qf[t][c + 1], s1, 0, 0, 0);
+        }
+        sc[st] = s0 + s1;
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float x = sc[i / 4][i % 4];
+        x = CAP ? capped(x, c1, c2) : x * sl2;
+        if (!full) {
+          const int j = k0 + i / 4 * 16 + 4 * grp + i % 4;
+          if (!sees(w[t].lim, j)) x = -INFINITY;
+          if (holes && (unsigned)it.pages[min(j, it.klim - 1) >> shift] >= (unsigned)a.kv.n_pages) x = -INFINITY;
+        }
+        sc[i / 4][i % 4] = x;
+        mx = vmax(mx, x);
+      }
+      mx = max_x32(max_x16(mx));
+      // (the reference follows only a growth of 2^8, as in softmax_tile)
+      if (__ballot(mx > m[t] + 8.f)) {
+        const float mn = vmax(m[t], mx), alpha = __builtin_amdgcn_exp2f(m[t] - (mn == -INFINITY ? 0.f : mn));
+        m[t] = mn;
+        l[t] *= alpha;
+#pragma unroll
+        for (int u2 = 0; u2 < ND; ++u2) o[t][u2] *= alpha;
+      }
+      const float ref = m[t] == -INFINITY ? 0.f : m[t];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = __builtin_amdgcn_exp2f(sc[i / 4][i % 4] - ref);
+        l[t] += x;
+        pf[t][i] = (bf16)x;
+      }
+    }
     // the values have landed once only the next keys' loads are pending
     if (next) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LK) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    bf16x8 vf[2][ND];
+    bf16x8 vf[ND];
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int u2 = 0; u2 < ND; ++u2) vf[c][u2] = read_vt<HDP>(va, u2, c * 16 * Y::ROWB);
+    for (int u2 = 0; u2 < ND; ++u2) {
+      const unsigned at = (va ^ (u2 % 8 << 5)) + u2 / 8 * 256;
+      vf[u2] = __builtin_shufflevector(read_tr(at), read_tr(at + 16 * Y::ROWB), 0, 1, 2, 3, 4, 5, 6, 7);
+    }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    if (next) mv.template load<false>(vb, nullptr, lds_addr(slot_v), 0);
+    if (next) mv.template load<false>(vb, nullptr, slot_v, 0);
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const bf16x8 pf = weights_of(sc[0], c);
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
-      for (int u2 = 0; u2 < ND; ++u2) s.o[u2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c][u2], pf, s.o[u2], 0, 0, 0);
-    }
+      for (int u2 = 0; u2 < ND; ++u2) o[t][u2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[u2], pf[t], o[t][u2], 0, 0, 0);
   }
-  s.l = sum_x32(s.l);
-  {
-    const int mine = it.uend - it.ubeg - wave;
-    repair<HDP, CAP>(a, it, s, qf, w.lim, sl2, c1, c2, mine > 0 ? (mine + NW - 1) / NW : 0, KT,
-                     [&](int n) { return first_key(it.ubeg + n * NW + wave); });
+  float z = 0.f;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    l[t] = sum_x32(sum_x16(l[t]));
+#pragma unroll
+    for (int u = 0; u < ND; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z = __builtin_fmaf(o[t][u][e], 0.f, z);
+  }
+  // rows with an output that is not finite: again, key by key (as `repair`)
+  if (__ballot(z != z) != 0) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const float ref = m[t] == -INFINITY ? 0.f : m[t];
+#pragma unroll
+      for (int u = 0; u < ND; ++u) o[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int u = it.ubeg + wave; u < it.uend; u += NW) {
+        const int k0 = first_key(u);
+#pragma unroll 1
+        for (int j = k0; j < min(k0 + KT, it.klim); ++j) {
+          const bool vis = sees(w[t].lim, j);
+          if (__ballot(vis) == 0) continue;
+          const long off = page_offset(a, it.pages[j >> shift], it.g);
+          if (off < 0) continue;
+          const long at = off + (long)(j & ((1 << shift) - 1)) * a.kv.tok_stride;
+          float d = 0.f;
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+            if (32 * c + 8 * grp < hd) {
+              const bf16x8 x = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const bf16*>(a.kv.k) + at + 32 * c + 8 * grp);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) d = __builtin_fmaf((float)x[e], (float)qf[t][c][e], d);
+            }
+          d = sum_x32(sum_x16(d));
+          const float pj = __builtin_amdgcn_exp2f((CAP ? capped(d, c1, c2) : d * sl2) - ref);
+#pragma unroll
+          for (int u2 = 0; u2 < ND; ++u2)
+            if (vis && 16 * u2 + 4 * grp < hd) {
+              const bf16x4 x = *reinterpret_cast<const bf16x4*>(reinterpret_cast<const bf16*>(a.kv.v) + at + 16 * u2 + 4 * grp);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[t][u2][e] = __builtin_fmaf(pj, (float)x[e], o[t][u2][e]);
+            }
+        }
+      }
+    }
   }
   // the waves store outputs and statistics, then each adds a quarter of the dims in wave order
   __syncthreads();
   f32x4* mo = reinterpret_cast<f32x4*>(smem);
 #pragma unroll
-  for (int u = 0; u < ND; ++u)
+  for (int t = 0; t < RT; ++t) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      mo[(wave * ND * 4 + u * 4 + q) * 64 + lane] = f32x4{s.o[u][4 * q], s.o[u][4 * q + 1], s.o[u][4 * q + 2], s.o[u][4 * q + 3]};
-  if (h == 0) {
-    stats[wave][lq][0] = s.m;
-    stats[wave][lq][1] = s.l;
+    for (int u = 0; u < ND; ++u) mo[((wave * RT + t) * ND + u) * 64 + lane] = o[t][u];
+    if (grp == 0) {
+      stats[wave][t * 16 + lq][0] = m[t];
+      stats[wave][t * 16 + lq][1] = l[t];
+    }
   }
   __syncthreads();
-  float m = -INFINITY, l = 0.f, wt[NW];
 #pragma unroll
-  for (int q = 0; q < NW; ++q) m = vmax(m, stats[q][lq][0]);
+  for (int t = 0; t < RT; ++t) {
+    const int row = t * 16 + lq;
+    float mm = -INFINITY, ll = 0.f, wt[NW];
 #pragma unroll
-  for (int q = 0; q < NW; ++q) {
-    // (a wave without keys weighs nothing)
-    wt[q] = stats[q][lq][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stats[q][lq][0] - m);
-    l += stats[q][lq][1] * wt[q];
-  }
-  if (it.row0 + lq >= it.nrows) return;
-  const float inv = inverse(l);
-#pragma unroll
-  for (int i = 0; i < ND; ++i) {
-    const int j = wave * ND + i;               // f32x4 j of the lane: subtile j / 4, group j % 4
-    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int q = 0; q < NW; ++q) mm = vmax(mm, stats[q][row][0]);
 #pragma unroll
     for (int q = 0; q < NW; ++q) {
-      const f32x4 x = mo[(q * ND * 4 + j) * 64 + lane];
-      if (wt[q] != 0.f) acc += x * wt[q];
+      // (a wave without keys weighs nothing)
+      wt[q] = stats[q][row][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stats[q][row][0] - mm);
+      ll += stats[q][row][1] * wt[q];
     }
-    put(a, it, w, direct, 32 * (j / 4) + 8 * (j % 4) + 4 * h, acc, inv);
+    if (it.row0 + row >= it.nrows) continue;
+    const float inv = inverse(ll);
+#pragma unroll
+    for (int i = 0; i < ND / NW; ++i) {
+      const int u = wave * (ND / NW) + i;
+      f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int q = 0; q < NW; ++q) {
+        const f32x4 x = mo[((q * RT + t) * ND + u) * 64 + lane];
+        if (wt[q] != 0.f) acc += x * wt[q];
+      }
+      put(a, it, w[t], direct, 16 * u + 4 * grp, acc, inv);
+    }
+    if (wave == 0 && grp == 0) put_stats(a, it, w[t], direct, mm, ll);
   }
-  if (wave == 0 && h == 0) put_stats(a, it, w, direct, m, l);
 }
 
 // ---------------------------------------------------------------- fp32
@@ -1063,13 +1180,13 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a) {
   const long row = blockIdx.x * (long)RB + tid / (LPR * WPR);
   const int tok = (int)(row / a.n_q), head = (int)(row - (long)tok * a.n_q);
   const float* stat = a.ws + (long)a.bt.n_tok * a.n_q * S * hd + row * S * 2;
-  // rows of no request, and those that are written already
-  bool live = tok < a.bt.n_tok && tok >= a.bt.start[0] && tok < a.bt.start[a.bt.n_req];
-  live = live && !(stat[1] < 0.f);
+  const bool in_rows = tok < a.bt.n_tok;
+  // rows of no request, and those that are written already (what their slots hold is read, and not used)
+  const bool live = in_rows && tok >= a.bt.start[0] && tok < a.bt.start[a.bt.n_req] && !(stat[1] < 0.f);
   const bool dok = sub * 4 < hd;
   float m = -INFINITY, l = 0.f;
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
-  for (int b = grp * N; live && b < S; b += WPR * N) {
+  for (int b = grp * N; in_rows && b < S; b += WPR * N) {
     float ms[N], ls[N];
     f32x4 pt[N];
 #pragma unroll
@@ -1134,9 +1251,11 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a) {
 // ---------------------------------------------------------------- host
 // Rows of a tile, keys of a key tile and key tiles of a round of kernel k at
 // padded head dim hdp.
-static int tile_rows(int k) { return k == PAGED_KEYS ? 32 : k == PAGED_F32 ? 16 : 128; }
-static int tile_keys(int k, int hdp) { return k == PAGED_KEYS ? 32 : k == PAGED_F32 ? 16 : hdp == 256 ? 32 : 64; }
-static int round_tiles(int k) { return k == PAGED_KEYS ? 4 : k == PAGED_ROWS2 ? 2 : 1; }
+static int tile_rows(int k) { return k == PAGED_KEYS2 ? 32 : k == PAGED_ROWS || k == PAGED_ROWS2 ? 128 : 16; }
+static int tile_keys(int k, int hdp) {
+  return k == PAGED_KEYS || k == PAGED_KEYS2 ? 32 : k == PAGED_F32 ? 16 : hdp == 256 ? 32 : 64;
+}
+static int round_tiles(int k) { return k == PAGED_KEYS || k == PAGED_KEYS2 ? 4 : k == PAGED_ROWS2 ? 2 : 1; }
 
 // Key ranges of a part: the count that minimises the time of a simple model:
 // waves of resident blocks times (start + rounds of tiles), and where a row has
@@ -1149,7 +1268,7 @@ static void cut(PagedPart& p, int hdp, int hd, int keys, int n_kv, long rows) {
   const double start = 3.0, merge = 3.0, bytes = 4.0 * kt * unit * hd;
   double best = 1e30;
   long best_per = total;
-  const long most = p.kernel == PAGED_KEYS || p.kernel == PAGED_F32 ? 256 : std::max<long>(1, resident / blocks);
+  const long most = p.kernel != PAGED_ROWS && p.kernel != PAGED_ROWS2 ? 256 : std::max<long>(1, resident / blocks);
   for (long s = 1; s <= std::min(total, most); ++s) {
     const long per = (total + s - 1) / s, n = (total + per - 1) / per;
     if (n != s) continue;
@@ -1170,7 +1289,11 @@ PagedPlan paged_plan(const PagedAttnArgs& a, int et) {
   const long all = (long)a.bt.n_tok * a.G;
   auto part = [&](long rows_req, bool flat, int keys) {
     PagedPart q{};
-    q.kernel = et == ET_F32 ? PAGED_F32 : (flat ? all : rows_req) <= 32 ? PAGED_KEYS : PAGED_ROWS;
+    q.kernel = et == ET_F32 ? PAGED_F32 : PAGED_ROWS;
+    if (et != ET_F32) {
+      const long r = flat ? all : rows_req;
+      q.kernel = r <= 16 ? PAGED_KEYS : r <= 32 ? PAGED_KEYS2 : PAGED_ROWS;
+    }
     const int br = tile_rows(q.kernel);
     q.tiles = (int)(flat ? std::max<long>(1, (all + br - 1) / br) : rows_req <= br ? a.bt.n_req : all / br + a.bt.n_req);
     if (q.kernel == PAGED_ROWS && (long)q.tiles * a.kv.n_kv <= 256) q.kernel = PAGED_ROWS2;
@@ -1199,7 +1322,8 @@ size_t paged_attention_ws(const PagedAttnArgs& a, int et) {
 template <int HDP, bool CAP>
 static void launch_part(const PagedAttnArgs& a, int kernel, hipStream_t s) {
   const dim3 grid((unsigned)a.tiles * a.kv.n_kv, a.ranges);
-  if (kernel == PAGED_KEYS) hipLaunchKernelGGL((paged_keys_kernel<HDP, CAP>), grid, dim3(256), 0, s, a);
+  if (kernel == PAGED_KEYS) hipLaunchKernelGGL((paged_keys_kernel<HDP, 1, CAP>), grid, dim3(256), 0, s, a);
+  else if (kernel == PAGED_KEYS2) hipLaunchKernelGGL((paged_keys_kernel<HDP, 2, CAP>), grid, dim3(256), 0, s, a);
   else if (kernel == PAGED_ROWS) hipLaunchKernelGGL((paged_rows_kernel<HDP, CAP, 1>), grid, dim3(256), 0, s, a);
   else if (kernel == PAGED_ROWS2) hipLaunchKernelGGL((paged_rows_kernel<HDP, CAP, 2>), grid, dim3(512), 0, s, a);
   else hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP>), grid, dim3(512), 0, s, a);
