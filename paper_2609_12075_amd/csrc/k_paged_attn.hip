@@ -41,7 +41,7 @@ struct Item {
   int g, r, row0, nrows, first, place0, len, prefix;
   int klim;                                    // keys from here on are not read
   int n1, t2, ntiles;                          // tile list: 0 .. n1 - 1, then t2 ..
-  int ubeg, uend, slot, nranges;
+  int ubeg, uend, slot;
   const int32_t* pages;
 };
 
@@ -63,7 +63,7 @@ __device__ __forceinline__ Limits limits(const PagedAttnArgs& a, int p, int len,
 template <int BR, int KT, int PAD>
 __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, Item& it) {
   const RaggedBatch& bt = a.bt;
-  const int L = blockIdx.x, v = L / a.kv.n_kv;
+  const int L = blockIdx.x, v = div_by(L, a.kv.n_kv, a.mul_kv);
   it.g = L - v * a.kv.n_kv;                    // KV heads fastest: with eight of them, one on each die
   // causal row tiles get longer: the long ones first
   const int tile = a.causal && !a.flat ? a.tiles - 1 - v : v;
@@ -79,7 +79,7 @@ __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, Item& it) {
     it.place0 = it.prefix = 0;
     it.pages = bt.pages;
     if (it.row0 >= it.nrows) return false;
-    it.n1 = it.ntiles = (a.khi - a.klo + KT - 1) / KT;
+    it.n1 = it.ntiles = (unsigned)(a.khi - a.klo + KT - 1) / KT;
     it.t2 = it.n1;
   } else {
     int t = 0;
@@ -113,14 +113,13 @@ __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, Item& it) {
     it.klim = min(sp.len, a.khi);
     it.pages = bt.pages + (long)it.r * bt.pages_stride;
     const int last = min(it.row0 + BR, it.nrows) - 1;
-    const Limits m0 = limits(a, it.place0 + it.row0 / a.G, it.len, it.prefix);
-    const Limits m1 = limits(a, it.place0 + last / a.G, it.len, it.prefix);
-    it.n1 = m0.pre > a.klo ? ((m0.pre - a.klo + KT - 1) / KT + PAD - 1) / PAD * PAD : 0;
-    it.t2 = max(it.n1, (m0.lo - a.klo) / KT);
-    const int t2e = m1.hi > a.klo ? (m1.hi - a.klo + KT - 1) / KT : 0;
+    const Limits m0 = limits(a, it.place0 + div_by(it.row0, a.G, a.mul_g), it.len, it.prefix);
+    const Limits m1 = limits(a, it.place0 + div_by(last, a.G, a.mul_g), it.len, it.prefix);
+    it.n1 = (unsigned)(max(0, m0.pre - a.klo) + KT * PAD - 1) / (KT * PAD) * PAD;
+    it.t2 = max(it.n1, (int)((unsigned)max(0, m0.lo - a.klo) / KT));
+    const int t2e = (unsigned)(max(0, m1.hi - a.klo) + KT - 1) / KT;
     it.ntiles = it.n1 + max(0, t2e - it.t2);
   }
-  it.nranges = (it.ntiles + a.chunk - 1) / a.chunk;
   it.ubeg = range * a.chunk;
   it.uend = min(it.ntiles, it.ubeg + a.chunk);
   return true;
@@ -131,7 +130,7 @@ struct Row { int tok, head; Limits lim; };
 // Row `row` of the item (rows behind the last one stand for the last one).
 __device__ __forceinline__ Row row_of(const PagedAttnArgs& a, const Item& it, int row) {
   Row w;
-  const int rc = min(row, it.nrows - 1), t = rc / a.G;
+  const int rc = min(row, it.nrows - 1), t = div_by(rc, a.G, a.mul_g);
   w.tok = it.first + t;
   w.head = it.g * a.G + rc - t * a.G;
   if (a.flat) {
@@ -219,7 +218,7 @@ __device__ __forceinline__ void empty_range(const PagedAttnArgs& a, const Item& 
   for (int i = threadIdx.x; i < BR; i += blockDim.x) {
     const int row = it.row0 + i;
     if (row >= it.nrows) break;
-    const int t = row / a.G;
+    const int t = div_by(row, a.G, a.mul_g);
     store_stats(a, (long)(it.first + t) * a.n_q + it.g * a.G + row - t * a.G, it.slot, -INFINITY, 0.f);
   }
 }
@@ -352,7 +351,9 @@ struct Mover {
     if (__ballot(ok) == ~0ull && shift >= __builtin_ctz(RS) && hd == HDP) {
       const int lo = (int)at, hi = (int)(at >> 32);
       const unsigned row = lrow * ts2;
-#pragma unroll
+      // (long unrolled code is read from memory in each launch: at a few
+      // cycles an instruction a loop of four is faster than 16 in a row)
+#pragma unroll 4
       for (int i = 0; i < N; ++i) {
         const unsigned j = i * NWV + wave, off = row + (piece ^ (((j * RS / Y::RP) & Y::SWM) << 4));
         const long b = (long)((unsigned long)(unsigned)__builtin_amdgcn_readlane(hi, i * RS) << 32 |
@@ -506,6 +507,18 @@ __device__ __forceinline__ void repair(const PagedAttnArgs& a, const Item& it, A
   }
 }
 
+// A lane's pieces of a query row: 8 dims every STEP; from `end` dims on zeros.
+template <int N, int STEP>
+__device__ __forceinline__ void load_q(const bf16* p, int end, bool whole, bf16x8 (&q)[N]) {
+  if (whole) {
+#pragma unroll
+    for (int c = 0; c < N; ++c) q[c] = *reinterpret_cast<const bf16x8*>(p + STEP * c);
+  } else {
+#pragma unroll
+    for (int c = 0; c < N; ++c) q[c] = STEP * c < end ? *reinterpret_cast<const bf16x8*>(p + STEP * c) : bf16x8{};
+  }
+}
+
 // The queries are in registers from here on (else the compiler, which does not
 // know the waits of the loop, waits for all loads before each use of them).
 template <int N>
@@ -554,7 +567,7 @@ __global__ void __launch_bounds__(256 * KS, 2) paged_rows_kernel(PagedAttnArgs a
   __shared__ float stats[KS][128][2];
   Item it;
   if (!find_item<128, KT, KS>(a, it)) return;
-  const bool direct = a.direct && it.nranges <= 1;
+  const bool direct = a.direct && it.ntiles <= a.chunk;
   if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
     if (!direct) empty_range<128>(a, it);
     return;
@@ -569,8 +582,7 @@ __global__ void __launch_bounds__(256 * KS, 2) paged_rows_kernel(PagedAttnArgs a
   bf16x8 qf[NC];
   {
     const bf16* qp = reinterpret_cast<const bf16*>(a.q) + (long)w.tok * a.q_ts + (long)w.head * a.q_hs;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) qf[c] = 16 * c + 8 * h < hd ? *reinterpret_cast<const bf16x8*>(qp + 16 * c + 8 * h) : bf16x8{};
+    load_q<NC, 16>(qp + 8 * h, hd - 8 * h, hd == HDP, qf);
   }
   Acc<HDP> s;
 #pragma unroll
@@ -723,7 +735,7 @@ __global__ void __launch_bounds__(256 * KS, 2) paged_rows_kernel(PagedAttnArgs a
 }
 
 // ---------------------------------------------------------------- bf16, waves split the keys
-// 16 RT rows a block; wave w takes every fourth tile of 32 keys into a K and a
+// 16 RT rows a block; wave w takes every fourth tile of 32 keys (16 at head dim 256) into a K and a
 // V slot of its own and waits for its own loads only: no barrier in the loop,
 // and a slot is loaded again as soon as its fragments are in registers. The
 // waves' (max, sum, output) meet in LDS at the end. For single tokens, whose
@@ -742,10 +754,18 @@ __device__ __forceinline__ float sum_x16(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// o += V^T P^T over the 32 or 16 keys of two fragments
+__device__ __forceinline__ f32x4 pv_mma(bf16x8 v, bf16x8 p, f32x4 o) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 pv_mma(bf16x4 v, bf16x4 p, f32x4 o) {
+  return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(v4s, v), __builtin_bit_cast(v4s, p), o, 0, 0, 0);
+}
+
 template <int HDP, int RT, bool CAP>
-__global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(PagedAttnArgs a) {
+__global__ void __launch_bounds__(256, HDP == 256 && RT == 2 ? 1 : 2) paged_keys_kernel(PagedAttnArgs a) {
   using Y = Lay<HDP>;
-  constexpr int KT = 32, NW = 4, NC = HDP / 32, ND = HDP / 16, TILE = KT * Y::ROWB, LK = TILE / 1024;
+  constexpr int KT = HDP == 256 ? 16 : 32, NST = KT / 16, NW = 4, NC = HDP / 32, ND = HDP / 16, TILE = KT * Y::ROWB, LK = TILE / 1024;
   constexpr int MERGE = NW * RT * ND * 1024;
   __shared__ __attribute__((aligned(1024))) char smem[NW * 2 * TILE > MERGE ? NW * 2 * TILE : MERGE];
   __shared__ Window win;
@@ -760,7 +780,7 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
   }
   Item it;
   if (!find_item<16 * RT, KT, NW>(a, it)) return;
-  const bool direct = a.direct && it.nranges <= 1;
+  const bool direct = a.direct && it.ntiles <= a.chunk;
   if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
     if (!direct) empty_range<16 * RT>(a, it);
     return;
@@ -778,11 +798,7 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
     wl = t == 0 ? x : WaveLimits{min(wl.pre0, x.pre0), max(wl.pre1, x.pre1), min(wl.lo0, x.lo0), max(wl.lo1, x.lo1),
                                  min(wl.hi0, x.hi0), max(wl.hi1, x.hi1)};
     const bf16* qp = reinterpret_cast<const bf16*>(a.q) + (long)w[t].tok * a.q_ts + (long)w[t].head * a.q_hs;
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-      qf[t][c] = 32 * c + 8 * grp < hd ? *reinterpret_cast<const bf16x8*>(qp + 32 * c + 8 * grp) : bf16x8{};
-#pragma unroll
-    for (int u = 0; u < ND; ++u) o[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    load_q<NC, 32>(qp + 8 * grp, hd - 8 * grp, hd == HDP, qf[t]);
     m[t] = -INFINITY;
     l[t] = 0.f;
   }
@@ -803,8 +819,15 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
       mv.template load<false>(vb, nullptr, slot_v, 0);
     }
   }
+  // (zeros while the loads are under way)
+  float zero = 0.f;
+  asm volatile("" : "+v"(zero));
 #pragma unroll
-  for (int t = 0; t < RT; ++t) hold(qf[t]);
+  for (int t = 0; t < RT; ++t) {
+#pragma unroll
+    for (int u = 0; u < ND; ++u) o[t][u] = f32x4{zero, zero, zero, zero};
+    hold(qf[t]);
+  }
   const unsigned ka = slot_k + lq * Y::ROWB + ((grp ^ Y::swz(lq)) << 4);
   const int vr = 4 * grp + (lq >> 2);
   const unsigned va = slot_v + vr * Y::ROWB + ((((lq & 3) >> 1) ^ Y::swz(vr)) << 4) + ((lq & 1) << 3);
@@ -824,9 +847,9 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
     if (u >= it.uend) continue;
     // this tile's keys have landed once only its values' loads are pending
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LK) : "memory");
-    bf16x8 kf[2][NC];
+    bf16x8 kf[NST][NC];
 #pragma unroll
-    for (int st = 0; st < 2; ++st)
+    for (int st = 0; st < NST; ++st)
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         typedef const __attribute__((address_space(3))) bf16x8* P;
@@ -839,12 +862,13 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
       mv.template load<false>(kb, nullptr, slot_k, 0);
     }
     const bool full = !holes && tile_full(wl, k0, k0 + KT);
-    bf16x8 pf[RT];
+    typedef __attribute__((ext_vector_type(4 * NST))) __bf16 frag;   // the keys of a lane
+    frag pf[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      f32x4 sc[2];
+      f32x4 sc[NST];
 #pragma unroll
-      for (int st = 0; st < 2; ++st) {
+      for (int st = 0; st < NST; ++st) {
         f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;         // two chains
 #pragma unroll
         for (int c = 0; c < NC; c += 2) {
@@ -855,7 +879,7 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
       }
       float mx = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < 4 * NST; ++i) {
         float x = sc[i / 4][i % 4];
         x = CAP ? capped(x, c1, c2) : x * sl2;
         if (!full) {
@@ -870,14 +894,17 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
       // (the reference follows only a growth of 2^8, as in softmax_tile)
       if (__ballot(mx > m[t] + 8.f)) {
         const float mn = vmax(m[t], mx), alpha = __builtin_amdgcn_exp2f(m[t] - (mn == -INFINITY ? 0.f : mn));
+        const bool some = __ballot(m[t] != -INFINITY) != 0;      // (else there is nothing yet to rescale)
         m[t] = mn;
         l[t] *= alpha;
+        if (some) {
 #pragma unroll
-        for (int u2 = 0; u2 < ND; ++u2) o[t][u2] *= alpha;
+          for (int u2 = 0; u2 < ND; ++u2) o[t][u2] *= alpha;
+        }
       }
       const float ref = m[t] == -INFINITY ? 0.f : m[t];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < 4 * NST; ++i) {
         const float x = __builtin_amdgcn_exp2f(sc[i / 4][i % 4] - ref);
         l[t] += x;
         pf[t][i] = (bf16)x;
@@ -886,11 +913,12 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
     // the values have landed once only the next keys' loads are pending
     if (next) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LK) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    bf16x8 vf[ND];
+    frag vf[ND];
 #pragma unroll
     for (int u2 = 0; u2 < ND; ++u2) {
       const unsigned at = (va ^ (u2 % 8 << 5)) + u2 / 8 * 256;
-      vf[u2] = __builtin_shufflevector(read_tr(at), read_tr(at + 16 * Y::ROWB), 0, 1, 2, 3, 4, 5, 6, 7);
+      if constexpr (NST == 2) vf[u2] = __builtin_shufflevector(read_tr(at), read_tr(at + 16 * Y::ROWB), 0, 1, 2, 3, 4, 5, 6, 7);
+      else vf[u2] = read_tr(at);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
@@ -898,7 +926,7 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
-      for (int u2 = 0; u2 < ND; ++u2) o[t][u2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[u2], pf[t], o[t][u2], 0, 0, 0);
+      for (int u2 = 0; u2 < ND; ++u2) o[t][u2] = pv_mma(vf[u2], pf[t], o[t][u2]);
   }
   float z = 0.f;
 #pragma unroll
@@ -974,15 +1002,13 @@ __global__ void __launch_bounds__(256, HDP == 256 ? 1 : 2) paged_keys_kernel(Pag
     }
     if (it.row0 + row >= it.nrows) continue;
     const float inv = inverse(ll);
+    // (a wave, or a row of it, without keys has stored zeros)
 #pragma unroll
     for (int i = 0; i < ND / NW; ++i) {
       const int u = wave * (ND / NW) + i;
-      f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+      f32x4 acc = mo[(t * ND + u) * 64 + lane] * wt[0];
 #pragma unroll
-      for (int q = 0; q < NW; ++q) {
-        const f32x4 x = mo[((q * RT + t) * ND + u) * 64 + lane];
-        if (wt[q] != 0.f) acc += x * wt[q];
-      }
+      for (int q = 1; q < NW; ++q) acc += mo[((q * RT + t) * ND + u) * 64 + lane] * wt[q];
       put(a, it, w[t], direct, 16 * u + 4 * grp, acc, inv);
     }
     if (wave == 0 && grp == 0) put_stats(a, it, w[t], direct, mm, ll);
@@ -999,7 +1025,7 @@ __global__ void __launch_bounds__(512) paged_f32_kernel(PagedAttnArgs a) {
   __shared__ __attribute__((aligned(16))) float mg[NW / 2][64 * REC];
   Item it;
   if (!find_item<16, KT, 1>(a, it)) return;
-  const bool direct = a.direct && it.nranges <= 1;
+  const bool direct = a.direct && it.ntiles <= a.chunk;
   if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
     if (!direct) empty_range<16>(a, it);
     return;
@@ -1253,7 +1279,8 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a) {
 // padded head dim hdp.
 static int tile_rows(int k) { return k == PAGED_KEYS2 ? 32 : k == PAGED_ROWS || k == PAGED_ROWS2 ? 128 : 16; }
 static int tile_keys(int k, int hdp) {
-  return k == PAGED_KEYS || k == PAGED_KEYS2 ? 32 : k == PAGED_F32 ? 16 : hdp == 256 ? 32 : 64;
+  const int wide = hdp == 256 ? 1 : 2;
+  return k == PAGED_F32 ? 16 : k == PAGED_KEYS || k == PAGED_KEYS2 ? 16 * wide : 32 * wide;
 }
 static int round_tiles(int k) { return k == PAGED_KEYS || k == PAGED_KEYS2 ? 4 : k == PAGED_ROWS2 ? 2 : 1; }
 
@@ -1346,6 +1373,7 @@ static void launch_merge(const PagedAttnArgs& a, int hdp, long rows, hipStream_t
 void launch_paged_attention(const PagedAttnArgs& a, int et, hipStream_t s) {
   if (a.bt.n_tok <= 0 || a.bt.max_new <= 0) return;
   const PagedPlan p = paged_plan(a, et);
+  auto mul = [](unsigned d) { return d == 1 ? 0u : (unsigned)(((1ull << 32) + d - 1) / d); };
   int slot = 0;
   for (int i = 0; i < p.n_parts; ++i) {
     const PagedPart& q = p.part[i];
@@ -1356,6 +1384,7 @@ void launch_paged_attention(const PagedAttnArgs& a, int et, hipStream_t s) {
     b.tiles = q.tiles; b.chunk = q.chunk; b.ranges = q.ranges;
     b.slot0 = slot; b.slots = p.slots;
     b.direct = p.n_parts == 1;
+    b.mul_g = mul(a.G); b.mul_kv = mul(a.kv.n_kv);
     slot += q.ranges;
     const bool cap = a.cap > 0.f;
     if (p.hdp == 64) cap ? launch_part<64, true>(b, q.kernel, s) : launch_part<64, false>(b, q.kernel, s);

@@ -49,6 +49,7 @@ struct PagedAttnArgs {
   int chunk;                                   // key tiles per range
   int ranges, slot0, slots;                    // ranges of this launch, its first slot, slots of a row
   int direct;                                  // rows whose keys fit one range are written at once
+  unsigned mul_g, mul_kv;                      // ceil(2^32 / d) for d = G and n_kv (0: d = 1)
 };
 
 // How an attention is computed. PAGED_KEYS: a block owns 16 rows (token, query
@@ -65,6 +66,14 @@ void launch_paged_attention(const PagedAttnArgs& a, int et, hipStream_t s);
 
 // ---------------------------------------------------------------- device side
 struct ReqSpan { int first, n, len; };         // first row, new tokens, tokens in the cache
+
+// n / d for mul = ceil(2^32 / d) and n < 2^31: the product's high word is the
+// quotient or one more.
+__device__ __forceinline__ int div_by(int n, int d, unsigned mul) {
+  if (mul == 0) return n;
+  const int q = (int)__umulhi((unsigned)n, mul);
+  return q - (q * d > n);
+}
 
 // Request r's rows and lengths, cut to the stated bounds.
 __device__ __forceinline__ ReqSpan span_of(const RaggedBatch& b, int r, int page_shift) {
