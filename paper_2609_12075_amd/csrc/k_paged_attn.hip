@@ -58,23 +58,30 @@ __device__ __forceinline__ Limits limits(const PagedAttnArgs& a, int p, int len,
   return m;
 }
 
-// false: nothing to do. KT keys a tile; lists of keys below the prefix are
-// padded to PAD tiles, so that PAD neighbours of a list are neighbours in the cache.
-template <int BR, int KT, int PAD>
-__device__ __forceinline__ bool find_item(const PagedAttnArgs& a, Item& it) {
+// Uniform reads of the batch's description: through the scalar cache, several
+// at a time (nobody writes them while a kernel runs).
+__device__ __forceinline__ int fetch(const int32_t* p, long i) {
+  typedef const __attribute__((address_space(4))) int32_t* C;
+  return *(C)(uintptr_t)(p + i);
+}
+
+// What block L (KV heads fastest: with eight of them, one on each die) and key
+// range `range` compute; false: nothing. KT keys a tile; lists of keys below
+// the prefix are padded to PAD tiles, so that PAD neighbours of a list are
+// neighbours in the cache. FLAT: the rows of the whole batch in one sequence of
+// tiles, over pages of request 0.
+template <int BR, int KT, int PAD, bool FLAT>
+__device__ __forceinline__ bool find_item(const PagedAttnArgs& a, int L, int range, Item& it) {
   const RaggedBatch& bt = a.bt;
-  const int L = blockIdx.x, v = div_by(L, a.kv.n_kv, a.mul_kv);
-  it.g = L - v * a.kv.n_kv;                    // KV heads fastest: with eight of them, one on each die
-  // causal row tiles get longer: the long ones first
-  const int tile = a.causal && !a.flat ? a.tiles - 1 - v : v;
-  const int range = blockIdx.y;
+  const int v = div_by(L, a.kv.n_kv, a.mul_kv);
+  it.g = L - v * a.kv.n_kv;
   it.slot = a.slot0 + range;
-  if (a.flat) {
-    const int s0 = max(0, bt.start[0]), s1 = min(bt.n_tok, bt.start[bt.n_req]);
+  if constexpr (FLAT) {
+    const int s0 = max(0, fetch(bt.start, 0)), s1 = min(bt.n_tok, fetch(bt.start, bt.n_req));
     it.r = 0;
     it.first = s0;
     it.nrows = (s1 - s0) * a.G;
-    it.row0 = tile * BR;
+    it.row0 = v * BR;
     it.len = it.klim = a.khi;
     it.place0 = it.prefix = 0;
     it.pages = bt.pages;
@@ -82,6 +89,8 @@ __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, Item& it) {
     it.n1 = it.ntiles = (unsigned)(a.khi - a.klo + KT - 1) / KT;
     it.t2 = it.n1;
   } else {
+    // causal row tiles get longer: the long ones first
+    const int tile = a.causal ? a.tiles - 1 - v : v;
     int t = 0;
     if (bt.max_new * a.G <= BR) {
       it.r = tile;
@@ -100,10 +109,12 @@ __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, Item& it) {
         n = min(step, end - lo);
       }
       it.r = __builtin_amdgcn_readfirstlane(lo);
-      t = tile - ((int)((long)bt.start[it.r] * a.G / BR) + it.r);
     }
-    it.prefix = a.prefix ? a.prefix[it.r] : 0;
-    const ReqSpan sp = span_of(bt, it.r, a.kv.page_shift);
+    const int s0 = fetch(bt.start, it.r), s1 = fetch(bt.start, it.r + 1), kl = fetch(bt.kv_len, it.r);
+    const int pf = fetch(a.prefix ? a.prefix : bt.kv_len, it.r);
+    it.prefix = a.prefix ? pf : 0;
+    if (bt.max_new * a.G > BR) t = tile - ((int)((long)s0 * a.G / BR) + it.r);
+    const ReqSpan sp = span_of(bt, s0, s1, kl, a.kv.page_shift);
     it.first = sp.first;
     it.nrows = sp.n * a.G;
     it.row0 = t * BR;
@@ -128,12 +139,13 @@ __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, Item& it) {
 struct Row { int tok, head; Limits lim; };
 
 // Row `row` of the item (rows behind the last one stand for the last one).
+template <bool FLAT>
 __device__ __forceinline__ Row row_of(const PagedAttnArgs& a, const Item& it, int row) {
   Row w;
   const int rc = min(row, it.nrows - 1), t = div_by(rc, a.G, a.mul_g);
   w.tok = it.first + t;
   w.head = it.g * a.G + rc - t * a.G;
-  if (a.flat) {
+  if constexpr (FLAT) {
     const int r = lane_request_of(a.bt, w.tok);
     const ReqSpan sp = span_of(a.bt, r, a.kv.page_shift);
     w.lim = limits(a, sp.len - sp.n + w.tok - sp.first, sp.len, a.prefix ? a.prefix[r] : 0);
@@ -150,10 +162,10 @@ __device__ __forceinline__ bool sees(const Limits& m, int j) {
 // The least and largest limits of a wave's rows, for the test of whole tiles.
 struct WaveLimits { int pre0, pre1, lo0, lo1, hi0, hi1; };
 
-template <int ROWS>
+template <int ROWS, bool FLAT>
 __device__ __forceinline__ WaveLimits wave_limits(const PagedAttnArgs& a, const Limits& m) {
   WaveLimits w;
-  if (a.flat) {
+  if constexpr (FLAT) {
     w = {m.pre, m.pre, m.lo, m.lo, m.hi, m.hi};
 #pragma unroll
     for (int o = ROWS / 2; o > 0; o >>= 1) {
@@ -507,37 +519,59 @@ __device__ __forceinline__ void repair(const PagedAttnArgs& a, const Item& it, A
   }
 }
 
-// A lane's pieces of a query row: 8 dims every STEP; from `end` dims on zeros.
+// A lane's pieces of a query row: 8 dims every STEP; pieces from `end` dims on
+// are not there (their loads read the row's first piece).
 template <int N, int STEP>
-__device__ __forceinline__ void load_q(const bf16* p, int end, bool whole, bf16x8 (&q)[N]) {
-  if (whole) {
+__device__ __forceinline__ void load_q(const bf16* row, int first, int end, bf16x8 (&q)[N]) {
 #pragma unroll
-    for (int c = 0; c < N; ++c) q[c] = *reinterpret_cast<const bf16x8*>(p + STEP * c);
-  } else {
-#pragma unroll
-    for (int c = 0; c < N; ++c) q[c] = STEP * c < end ? *reinterpret_cast<const bf16x8*>(p + STEP * c) : bf16x8{};
+  for (int c = 0; c < N; ++c) {
+    const int d = first + STEP * c;
+    q[c] = *reinterpret_cast<const bf16x8*>(row + (d < end ? d : 0));
   }
 }
-
 // The queries are in registers from here on (else the compiler, which does not
-// know the waits of the loop, waits for all loads before each use of them).
-template <int N>
-__device__ __forceinline__ void hold(bf16x8 (&q)[N]) {
+// know the waits of the loop, waits for all loads before each use of them), and
+// pieces that are not there are zeros.
+template <int N, int STEP>
+__device__ __forceinline__ void hold(int first, int end, bool whole, bf16x8 (&q)[N]) {
 #pragma unroll
   for (int c = 0; c < N; ++c) asm volatile("" : "+v"(q[c]));
+  if (!whole) {
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+      if (first + STEP * c >= end) q[c] = bf16x8{};
+  }
+}
+// The kernel's arguments that are needed late are requested with the first.
+__device__ __forceinline__ void touch(const PagedAttnArgs& a) {
+  asm volatile("" ::"s"(a.q), "s"(a.q_ts), "s"(a.q_hs), "s"(a.kv.k), "s"(a.kv.v), "s"(a.kv.page_stride),
+               "s"(a.kv.head_stride), "s"(a.kv.tok_stride));
+  asm volatile("" ::"s"(a.scale), "s"(a.cap), "s"(a.window), "s"(a.ws), "s"(a.slots), "s"(a.o), "s"(a.o_ts), "s"(a.o_hs));
 }
 
 __device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
-// Four dims of a row: to the output, or to the range's slot.
-__device__ __forceinline__ void put(const PagedAttnArgs& a, const Item& it, const Row& w, bool direct, int dim, f32x4 v,
-                                    float inv) {
-  if (dim >= a.kv.hd) return;
+// N times four dims of a row, at dim(i) and of the value val(i): to the output,
+// or to the range's slot.
+template <int HDP, int N, typename Dim, typename Val>
+__device__ __forceinline__ void put(const PagedAttnArgs& a, const Item& it, const Row& w, bool direct, float inv, Dim dim,
+                                    Val val) {
+  const bool whole = a.kv.hd == HDP;
   if (direct) {
-    bf16* op = reinterpret_cast<bf16*>(a.o) + (long)w.tok * a.o_ts + (long)w.head * a.o_hs + dim;
-    *reinterpret_cast<bf16x4*>(op) = bf16x4{(bf16)(v[0] * inv), (bf16)(v[1] * inv), (bf16)(v[2] * inv), (bf16)(v[3] * inv)};
+    bf16* op = reinterpret_cast<bf16*>(a.o) + (long)w.tok * a.o_ts + (long)w.head * a.o_hs;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const f32x4 v = val(i) * inv;
+      if (whole || dim(i) < a.kv.hd)
+        *reinterpret_cast<bf16x4*>(op + dim(i)) = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+    }
   } else {
-    *reinterpret_cast<f32x4*>(part_of(a, (long)w.tok * a.n_q + w.head, it.slot) + dim) = v;
+    float* pp = part_of(a, (long)w.tok * a.n_q + w.head, it.slot);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const f32x4 v = val(i);
+      if (whole || dim(i) < a.kv.hd) *reinterpret_cast<f32x4*>(pp + dim(i)) = v;
+    }
   }
 }
 // The statistics of a row (one lane of it calls this). direct: the row's log-sum-exp.
@@ -556,17 +590,26 @@ __device__ __forceinline__ void put_stats(const PagedAttnArgs& a, const Item& it
 // tile, whose four waves load it together, through a ring of two rounds. (64
 // keys a tile; 32 at head dim 256.) Two groups where the blocks are few: their
 // results meet in LDS.
-template <int HDP, bool CAP, int KS>
-__global__ void __launch_bounds__(256 * KS, 2) paged_rows_kernel(PagedAttnArgs a) {
+template <int HDP, int KS>
+struct RowsShared {
+  static constexpr int KT = HDP == 256 ? 32 : 64, RING = 2 * KS * 2 * KT * Lay<HDP>::ROWB;
+  static constexpr int MERGE = KS > 1 ? 256 * HDP * 2 : 0;       // half of each group's outputs
+  __attribute__((aligned(1024))) char mem[RING > MERGE ? RING : MERGE];
+  Window win;
+  float stats[KS][128][2];
+};
+
+template <int HDP, bool CAP, int KS, bool FLAT>
+__device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP, KS>& sh, int L, int range) {
   using Y = Lay<HDP>;
-  constexpr int KT = HDP == 256 ? 32 : 64, NS = KT / 32, NC = HDP / 16, ND = HDP / 32;
+  constexpr int KT = RowsShared<HDP, KS>::KT, NS = KT / 32, NC = HDP / 16, ND = HDP / 32;
   constexpr int TILE = KT * Y::ROWB, ROUND = KS * 2 * TILE;
-  constexpr int MERGE = KS > 1 ? 256 * HDP * 2 : 0;       // half of each group's outputs
-  __shared__ __attribute__((aligned(1024))) char smem[2 * ROUND > MERGE ? 2 * ROUND : MERGE];
-  __shared__ Window win;
-  __shared__ float stats[KS][128][2];
+  char* smem = sh.mem;
+  Window& win = sh.win;
+  auto& stats = sh.stats;
+  touch(a);
   Item it;
-  if (!find_item<128, KT, KS>(a, it)) return;
+  if (!find_item<128, KT, KS, FLAT>(a, L, range, it)) return;
   const bool direct = a.direct && it.ntiles <= a.chunk;
   if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
     if (!direct) empty_range<128>(a, it);
@@ -577,12 +620,12 @@ __global__ void __launch_bounds__(256 * KS, 2) paged_rows_kernel(PagedAttnArgs a
   const int lq = lane & 31, h = lane >> 5, hd = a.kv.hd, shift = a.kv.page_shift;
   const int wrow = it.row0 + wr * 32;
   const bool active = wrow < it.nrows;
-  const Row w = row_of(a, it, wrow + lq);
-  const WaveLimits wl = wave_limits<32>(a, w.lim);
+  const Row w = row_of<FLAT>(a, it, wrow + lq);
+  const WaveLimits wl = wave_limits<32, FLAT>(a, w.lim);
   bf16x8 qf[NC];
   {
     const bf16* qp = reinterpret_cast<const bf16*>(a.q) + (long)w.tok * a.q_ts + (long)w.head * a.q_hs;
-    load_q<NC, 16>(qp + 8 * h, hd - 8 * h, hd == HDP, qf);
+    load_q<NC, 16>(qp, 8 * h, hd, qf);
   }
   Acc<HDP> s;
 #pragma unroll
@@ -612,7 +655,7 @@ __global__ void __launch_bounds__(256 * KS, 2) paged_rows_kernel(PagedAttnArgs a
     holes = fill_window<256 * KS>(a, it, win, w0);
     issue(0);
   }
-  hold(qf);
+  hold<NC, 16>(8 * h, hd, hd == HDP, qf);
   // where the lane's K and V fragments begin; the swizzled pieces of a row
   // differ in address bits only, which costs an instruction a read and no
   // registers (held for all pieces they spill at head dim 256)
@@ -711,13 +754,13 @@ __global__ void __launch_bounds__(256 * KS, 2) paged_rows_kernel(PagedAttnArgs a
     const float l = kg == 0 ? s.l * w1 + l2 * w2 : l2 * w2 + s.l * w1, inv = inverse(l);
     auto finish = [&](auto from) {
       constexpr int U = decltype(from)::value;
-#pragma unroll
-      for (int j = 0; j < ND * 2; ++j) {
-        const f32x16& x = s.o[U + j / 4];
-        const f32x4 mine = f32x4{x[4 * (j % 4)], x[4 * (j % 4) + 1], x[4 * (j % 4) + 2], x[4 * (j % 4) + 3]} * w1;
-        const f32x4 y = w2 == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : mo[slot(1 - kg, j)] * w2;
-        put(a, it, w, direct, 32 * (U + j / 4) + 8 * (j % 4) + 4 * h, mine + y, inv);
-      }
+      put<HDP, ND * 2>(a, it, w, direct, inv, [&](int j) { return 32 * (U + j / 4) + 8 * (j % 4) + 4 * h; },
+                       [&](int j) {
+                         const f32x16& x = s.o[U + j / 4];
+                         // (a group without keys has handed over zeros)
+                         return f32x4{x[4 * (j % 4)], x[4 * (j % 4) + 1], x[4 * (j % 4) + 2], x[4 * (j % 4) + 3]} * w1 +
+                                mo[slot(1 - kg, j)] * w2;
+                       });
     };
     if (kg == 0) finish(std::integral_constant<int, 0>{});
     else finish(std::integral_constant<int, ND / 2>{});
@@ -726,11 +769,10 @@ __global__ void __launch_bounds__(256 * KS, 2) paged_rows_kernel(PagedAttnArgs a
   }
   if (wrow + lq >= it.nrows) return;
   const float inv = inverse(s.l);
-#pragma unroll
-  for (int u = 0; u < ND; ++u)
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      put(a, it, w, direct, 32 * u + 8 * q + 4 * h, f32x4{s.o[u][4 * q], s.o[u][4 * q + 1], s.o[u][4 * q + 2], s.o[u][4 * q + 3]}, inv);
+  put<HDP, ND * 4>(a, it, w, direct, inv, [&](int j) { return 32 * (j / 4) + 8 * (j % 4) + 4 * h; }, [&](int j) {
+    const f32x16& x = s.o[j / 4];
+    return f32x4{x[4 * (j % 4)], x[4 * (j % 4) + 1], x[4 * (j % 4) + 2], x[4 * (j % 4) + 3]};
+  });
   if (h == 0) put_stats(a, it, w, direct, s.m, s.l);
 }
 
@@ -762,24 +804,34 @@ __device__ __forceinline__ f32x4 pv_mma(bf16x4 v, bf16x4 p, f32x4 o) {
   return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(v4s, v), __builtin_bit_cast(v4s, p), o, 0, 0, 0);
 }
 
-template <int HDP, int RT, bool CAP>
-__global__ void __launch_bounds__(256, HDP == 256 && RT == 2 ? 1 : 2) paged_keys_kernel(PagedAttnArgs a) {
+template <int HDP, int RT>
+struct KeysShared {
+  static constexpr int KT = HDP == 256 ? 16 : 32, NW = 4;
+  static constexpr int SLOTS = NW * 2 * KT * Lay<HDP>::ROWB, MERGE = NW * RT * HDP / 16 * 1024;
+  __attribute__((aligned(1024))) char mem[SLOTS > MERGE ? SLOTS : MERGE];
+  Window win;
+  float stats[NW][16 * RT][2];
+};
+
+template <int HDP, int RT, bool CAP, bool FLAT>
+__device__ __forceinline__ void keys_body(const PagedAttnArgs& a, KeysShared<HDP, RT>& sh, int L, int range) {
   using Y = Lay<HDP>;
-  constexpr int KT = HDP == 256 ? 16 : 32, NST = KT / 16, NW = 4, NC = HDP / 32, ND = HDP / 16, TILE = KT * Y::ROWB, LK = TILE / 1024;
-  constexpr int MERGE = NW * RT * ND * 1024;
-  __shared__ __attribute__((aligned(1024))) char smem[NW * 2 * TILE > MERGE ? NW * 2 * TILE : MERGE];
-  __shared__ Window win;
-  __shared__ float stats[NW][16 * RT][2];
+  constexpr int KT = KeysShared<HDP, RT>::KT, NST = KT / 16, NW = 4, NC = HDP / 32, ND = HDP / 16;
+  constexpr int TILE = KT * Y::ROWB, LK = TILE / 1024;
+  char* smem = sh.mem;
+  Window& win = sh.win;
+  auto& stats = sh.stats;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), shift = a.kv.page_shift;
+  touch(a);
   // the page numbers that the range needs if no window moves it: requested with the batch's lengths
-  const int guess = (a.klo + (int)blockIdx.y * a.chunk * KT) >> shift;
+  const int guess = (a.klo + range * a.chunk * KT) >> shift;
   int guessed = 0;
   if (a.bt.pages_stride > 0) {
-    const int tile = (int)blockIdx.x / a.kv.n_kv, r = a.flat ? 0 : (a.causal ? a.tiles - 1 - tile : tile);
+    const int tile = div_by(L, a.kv.n_kv, a.mul_kv), r = FLAT ? 0 : (a.causal ? a.tiles - 1 - tile : tile);
     guessed = a.bt.pages[(long)r * a.bt.pages_stride + min(guess + tid, a.bt.pages_stride - 1)];
   }
   Item it;
-  if (!find_item<16 * RT, KT, NW>(a, it)) return;
+  if (!find_item<16 * RT, KT, NW, FLAT>(a, L, range, it)) return;
   const bool direct = a.direct && it.ntiles <= a.chunk;
   if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
     if (!direct) empty_range<16 * RT>(a, it);
@@ -793,12 +845,12 @@ __global__ void __launch_bounds__(256, HDP == 256 && RT == 2 ? 1 : 2) paged_keys
   float m[RT], l[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    w[t] = row_of(a, it, it.row0 + t * 16 + lq);
-    const WaveLimits x = wave_limits<16>(a, w[t].lim);
+    w[t] = row_of<FLAT>(a, it, it.row0 + t * 16 + lq);
+    const WaveLimits x = wave_limits<16, FLAT>(a, w[t].lim);
     wl = t == 0 ? x : WaveLimits{min(wl.pre0, x.pre0), max(wl.pre1, x.pre1), min(wl.lo0, x.lo0), max(wl.lo1, x.lo1),
                                  min(wl.hi0, x.hi0), max(wl.hi1, x.hi1)};
     const bf16* qp = reinterpret_cast<const bf16*>(a.q) + (long)w[t].tok * a.q_ts + (long)w[t].head * a.q_hs;
-    load_q<NC, 32>(qp + 8 * grp, hd - 8 * grp, hd == HDP, qf[t]);
+    load_q<NC, 32>(qp, 8 * grp, hd, qf[t]);
     m[t] = -INFINITY;
     l[t] = 0.f;
   }
@@ -826,7 +878,7 @@ __global__ void __launch_bounds__(256, HDP == 256 && RT == 2 ? 1 : 2) paged_keys
   for (int t = 0; t < RT; ++t) {
 #pragma unroll
     for (int u = 0; u < ND; ++u) o[t][u] = f32x4{zero, zero, zero, zero};
-    hold(qf[t]);
+    hold<NC, 32>(8 * grp, hd, hd == HDP, qf[t]);
   }
   const unsigned ka = slot_k + lq * Y::ROWB + ((grp ^ Y::swz(lq)) << 4);
   const int vr = 4 * grp + (lq >> 2);
@@ -1003,15 +1055,59 @@ __global__ void __launch_bounds__(256, HDP == 256 && RT == 2 ? 1 : 2) paged_keys
     if (it.row0 + row >= it.nrows) continue;
     const float inv = inverse(ll);
     // (a wave, or a row of it, without keys has stored zeros)
+    const f32x4* mine = mo + (t * ND + wave * (ND / NW)) * 64 + lane;
+    put<HDP, ND / NW>(a, it, w[t], direct, inv, [&](int i) { return 16 * (wave * (ND / NW) + i) + 4 * grp; }, [&](int i) {
+      f32x4 acc = mine[i * 64] * wt[0];
 #pragma unroll
-    for (int i = 0; i < ND / NW; ++i) {
-      const int u = wave * (ND / NW) + i;
-      f32x4 acc = mo[(t * ND + u) * 64 + lane] * wt[0];
-#pragma unroll
-      for (int q = 1; q < NW; ++q) acc += mo[((q * RT + t) * ND + u) * 64 + lane] * wt[q];
-      put(a, it, w[t], direct, 16 * u + 4 * grp, acc, inv);
-    }
+      for (int q = 1; q < NW; ++q) acc += mine[(q * RT * ND + i) * 64] * wt[q];
+      return acc;
+    });
     if (wave == 0 && grp == 0) put_stats(a, it, w[t], direct, mm, ll);
+  }
+}
+
+// ---------------------------------------------------------------- bf16 kernels
+// KIND: PagedKernel of the whole attention, or, for a batch with a common
+// context, of that (all rows in one sequence of tiles, the grid's first
+// blocks) and KIND2 of what follows it: the two do not wait for each other.
+template <int HDP, bool CAP, int KIND>
+__global__ void __launch_bounds__(KIND == PAGED_ROWS2 ? 512 : 256, KIND == PAGED_KEYS2 && HDP == 256 ? 1 : 2)
+    paged_kernel(PagedAttnArgs a) {
+  if constexpr (KIND == PAGED_ROWS || KIND == PAGED_ROWS2) {
+    __shared__ RowsShared<HDP, KIND == PAGED_ROWS2 ? 2 : 1> sh;
+    rows_body<HDP, CAP, KIND == PAGED_ROWS2 ? 2 : 1, false>(a, sh, blockIdx.x, blockIdx.y);
+  } else {
+    __shared__ KeysShared<HDP, KIND == PAGED_KEYS2 ? 2 : 1> sh;
+    keys_body<HDP, KIND == PAGED_KEYS2 ? 2 : 1, CAP, false>(a, sh, blockIdx.x, blockIdx.y);
+  }
+}
+
+template <int HDP, bool CAP, int KIND, int KIND2>
+__global__ void __launch_bounds__(256, (KIND == PAGED_KEYS2 || KIND2 == PAGED_KEYS2) && HDP == 256 ? 1 : 2)
+    paged_pair_kernel(PagedAttnArgs a, PagedAttnArgs b) {
+  union Shared {
+    RowsShared<HDP, 1> rows;
+    KeysShared<HDP, 1> keys;
+    KeysShared<HDP, KIND == PAGED_KEYS2 || KIND2 == PAGED_KEYS2 ? 2 : 1> keys2;
+  };
+  __shared__ __attribute__((aligned(1024))) char mem[sizeof(Shared)];
+  Shared& sh = *reinterpret_cast<Shared*>(mem);
+  const int per_a = a.tiles * a.kv.n_kv, na = per_a * a.ranges;
+  int L = blockIdx.x;
+  if (L < na) {
+    const int range = div_by(L, per_a, a.mul_blocks);
+    L -= range * per_a;
+    if constexpr (KIND == PAGED_ROWS) rows_body<HDP, CAP, 1, true>(a, sh.rows, L, range);
+    else if constexpr (KIND == PAGED_KEYS) keys_body<HDP, 1, CAP, true>(a, sh.keys, L, range);
+    else keys_body<HDP, 2, CAP, true>(a, sh.keys2, L, range);
+  } else {
+    const int per_b = b.tiles * b.kv.n_kv;
+    L -= na;
+    const int range = div_by(L, per_b, b.mul_blocks);
+    L -= range * per_b;
+    if constexpr (KIND2 == PAGED_ROWS) rows_body<HDP, CAP, 1, false>(b, sh.rows, L, range);
+    else if constexpr (KIND2 == PAGED_KEYS) keys_body<HDP, 1, CAP, false>(b, sh.keys, L, range);
+    else keys_body<HDP, 2, CAP, false>(b, sh.keys2, L, range);
   }
 }
 
@@ -1019,12 +1115,12 @@ __global__ void __launch_bounds__(256, HDP == 256 && RT == 2 ? 1 : 2) paged_keys
 // 16 rows a block, eight waves split the tiles of 16 keys; both products on
 // v_mfma_f32_16x16x4_f32 with operands straight from global memory. A tile's
 // page numbers are requested while the tile before is computed.
-template <int HDP, bool CAP>
+template <int HDP, bool CAP, bool FLAT>
 __global__ void __launch_bounds__(512) paged_f32_kernel(PagedAttnArgs a) {
   constexpr int NW = 8, KT = 16, NC = HDP / 16, REC = HDP / 4 + 4;
   __shared__ __attribute__((aligned(16))) float mg[NW / 2][64 * REC];
   Item it;
-  if (!find_item<16, KT, 1>(a, it)) return;
+  if (!find_item<16, KT, 1, FLAT>(a, blockIdx.x, blockIdx.y, it)) return;
   const bool direct = a.direct && it.ntiles <= a.chunk;
   if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
     if (!direct) empty_range<16>(a, it);
@@ -1032,7 +1128,7 @@ __global__ void __launch_bounds__(512) paged_f32_kernel(PagedAttnArgs a) {
   }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 15, lk = lane >> 4, hd = a.kv.hd, shift = a.kv.page_shift, smask = (1 << shift) - 1;
-  const Row w = row_of(a, it, it.row0 + lr);
+  const Row w = row_of<FLAT>(a, it, it.row0 + lr);
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   const float* qp = reinterpret_cast<const float*>(a.q) + (long)w.tok * a.q_ts + (long)w.head * a.q_hs;
   f32x4 qf[NC], o[NC];
@@ -1323,7 +1419,7 @@ PagedPlan paged_plan(const PagedAttnArgs& a, int et) {
     }
     const int br = tile_rows(q.kernel);
     q.tiles = (int)(flat ? std::max<long>(1, (all + br - 1) / br) : rows_req <= br ? a.bt.n_req : all / br + a.bt.n_req);
-    if (q.kernel == PAGED_ROWS && (long)q.tiles * a.kv.n_kv <= 256) q.kernel = PAGED_ROWS2;
+    if (q.kernel == PAGED_ROWS && a.shared_len == 0 && (long)q.tiles * a.kv.n_kv <= 256) q.kernel = PAGED_ROWS2;
     cut(q, p.hdp, a.kv.hd, keys, a.kv.n_kv, (long)a.bt.n_tok * a.n_q);
     return q;
   };
@@ -1347,13 +1443,43 @@ size_t paged_attention_ws(const PagedAttnArgs& a, int et) {
 }
 
 template <int HDP, bool CAP>
-static void launch_part(const PagedAttnArgs& a, int kernel, hipStream_t s) {
+static void launch_one(const PagedAttnArgs& a, int kernel, bool flat, hipStream_t s) {
   const dim3 grid((unsigned)a.tiles * a.kv.n_kv, a.ranges);
-  if (kernel == PAGED_KEYS) hipLaunchKernelGGL((paged_keys_kernel<HDP, 1, CAP>), grid, dim3(256), 0, s, a);
-  else if (kernel == PAGED_KEYS2) hipLaunchKernelGGL((paged_keys_kernel<HDP, 2, CAP>), grid, dim3(256), 0, s, a);
-  else if (kernel == PAGED_ROWS) hipLaunchKernelGGL((paged_rows_kernel<HDP, CAP, 1>), grid, dim3(256), 0, s, a);
-  else if (kernel == PAGED_ROWS2) hipLaunchKernelGGL((paged_rows_kernel<HDP, CAP, 2>), grid, dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP>), grid, dim3(512), 0, s, a);
+  if (kernel == PAGED_KEYS) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_KEYS>), grid, dim3(256), 0, s, a);
+  else if (kernel == PAGED_KEYS2) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_KEYS2>), grid, dim3(256), 0, s, a);
+  else if (kernel == PAGED_ROWS) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_ROWS>), grid, dim3(256), 0, s, a);
+  else if (kernel == PAGED_ROWS2) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_ROWS2>), grid, dim3(512), 0, s, a);
+  else if (flat) hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP, true>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP, false>), grid, dim3(512), 0, s, a);
+}
+
+// The two parts of a batch with a common context. (a request's rows are some
+// of the batch's, so the second part has no more rows a tile than the first)
+template <int HDP, bool CAP>
+static void launch_pair(const PagedAttnArgs& a, const PagedAttnArgs& b, int ka, int kb, hipStream_t s) {
+  const dim3 grid((unsigned)(a.tiles * a.kv.n_kv * a.ranges + b.tiles * b.kv.n_kv * b.ranges));
+#define PAIR(A, B) hipLaunchKernelGGL((paged_pair_kernel<HDP, CAP, A, B>), grid, dim3(256), 0, s, a, b)
+  if (ka == PAGED_ROWS) {
+    if (kb == PAGED_ROWS) PAIR(PAGED_ROWS, PAGED_ROWS);
+    else if (kb == PAGED_KEYS2) PAIR(PAGED_ROWS, PAGED_KEYS2);
+    else PAIR(PAGED_ROWS, PAGED_KEYS);
+  } else if (ka == PAGED_KEYS2) {
+    if (kb == PAGED_KEYS2) PAIR(PAGED_KEYS2, PAGED_KEYS2);
+    else PAIR(PAGED_KEYS2, PAGED_KEYS);
+  } else {
+    PAIR(PAGED_KEYS, PAGED_KEYS);
+  }
+#undef PAIR
+}
+
+template <int HDP, bool CAP>
+static void launch_parts(const PagedAttnArgs (&a)[2], const PagedPlan& p, hipStream_t s) {
+  const int ka = p.part[0].kernel, kb = p.part[1].kernel;
+  if (p.n_parts == 2 && ka != PAGED_F32) {
+    launch_pair<HDP, CAP>(a[0], a[1], ka, kb, s);
+    return;
+  }
+  for (int i = 0; i < p.n_parts; ++i) launch_one<HDP, CAP>(a[i], p.part[i].kernel, p.n_parts == 2 && i == 0, s);
 }
 
 template <typename T, int LPR>
@@ -1373,24 +1499,25 @@ static void launch_merge(const PagedAttnArgs& a, int hdp, long rows, hipStream_t
 void launch_paged_attention(const PagedAttnArgs& a, int et, hipStream_t s) {
   if (a.bt.n_tok <= 0 || a.bt.max_new <= 0) return;
   const PagedPlan p = paged_plan(a, et);
-  auto mul = [](unsigned d) { return d == 1 ? 0u : (unsigned)(((1ull << 32) + d - 1) / d); };
+  auto mul = [](long d) { return d == 1 ? 0u : (unsigned)(((1ull << 32) + d - 1) / d); };
+  PagedAttnArgs part[2] = {a, a};
   int slot = 0;
   for (int i = 0; i < p.n_parts; ++i) {
     const PagedPart& q = p.part[i];
-    PagedAttnArgs b = a;
-    b.flat = p.n_parts == 2 && i == 0;
+    PagedAttnArgs& b = part[i];
+    const bool flat = p.n_parts == 2 && i == 0;
     b.klo = p.n_parts == 2 && i == 1 ? a.shared_len : 0;
-    b.khi = b.flat ? a.shared_len : 1 << 30;
+    b.khi = flat ? a.shared_len : 1 << 30;
     b.tiles = q.tiles; b.chunk = q.chunk; b.ranges = q.ranges;
     b.slot0 = slot; b.slots = p.slots;
     b.direct = p.n_parts == 1;
-    b.mul_g = mul(a.G); b.mul_kv = mul(a.kv.n_kv);
+    b.mul_g = mul(a.G); b.mul_kv = mul(a.kv.n_kv); b.mul_blocks = mul((long)q.tiles * a.kv.n_kv);
     slot += q.ranges;
-    const bool cap = a.cap > 0.f;
-    if (p.hdp == 64) cap ? launch_part<64, true>(b, q.kernel, s) : launch_part<64, false>(b, q.kernel, s);
-    else if (p.hdp == 128) cap ? launch_part<128, true>(b, q.kernel, s) : launch_part<128, false>(b, q.kernel, s);
-    else cap ? launch_part<256, true>(b, q.kernel, s) : launch_part<256, false>(b, q.kernel, s);
   }
+  const bool cap = a.cap > 0.f;
+  if (p.hdp == 64) cap ? launch_parts<64, true>(part, p, s) : launch_parts<64, false>(part, p, s);
+  else if (p.hdp == 128) cap ? launch_parts<128, true>(part, p, s) : launch_parts<128, false>(part, p, s);
+  else cap ? launch_parts<256, true>(part, p, s) : launch_parts<256, false>(part, p, s);
   if (p.slots > 1) {
     PagedAttnArgs b = a;
     b.slots = p.slots;

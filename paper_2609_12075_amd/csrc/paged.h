@@ -44,12 +44,11 @@ struct PagedAttnArgs {
   float* ws;
   // set by the launcher, per launch
   int klo, khi;                                // keys [klo, khi) only
-  int flat;                                    // rows of the whole batch in one sequence of tiles, pages of request 0
   int tiles;                                   // row tiles of the grid
   int chunk;                                   // key tiles per range
   int ranges, slot0, slots;                    // ranges of this launch, its first slot, slots of a row
   int direct;                                  // rows whose keys fit one range are written at once
-  unsigned mul_g, mul_kv;                      // ceil(2^32 / d) for d = G and n_kv (0: d = 1)
+  unsigned mul_g, mul_kv, mul_blocks;          // ceil(2^32 / d) for d = G, n_kv and tiles * n_kv (0: d = 1)
 };
 
 // How an attention is computed. PAGED_KEYS: a block owns 16 rows (token, query
@@ -75,9 +74,9 @@ __device__ __forceinline__ int div_by(int n, int d, unsigned mul) {
   return q - (q * d > n);
 }
 
-// Request r's rows and lengths, cut to the stated bounds.
-__device__ __forceinline__ ReqSpan span_of(const RaggedBatch& b, int r, int page_shift) {
-  const int s0 = b.start[r], s1 = b.start[r + 1];
+// A request's rows and lengths from start[r], start[r + 1] and kv_len[r], cut to
+// the stated bounds.
+__device__ __forceinline__ ReqSpan span_of(const RaggedBatch& b, int s0, int s1, int len, int page_shift) {
   ReqSpan p;
   p.first = s0 < 0 ? 0 : (s0 > b.n_tok ? b.n_tok : s0);
   const int e = s1 > b.n_tok ? b.n_tok : s1;
@@ -85,11 +84,14 @@ __device__ __forceinline__ ReqSpan span_of(const RaggedBatch& b, int r, int page
   if (p.n > b.max_new) p.n = b.max_new;
   if (p.n < 0) p.n = 0;
   const long cap = (long)b.pages_stride << page_shift;
-  int len = b.kv_len[r];
   if (len > b.max_len) len = b.max_len;
   if (len > cap) len = (int)cap;
   p.len = len < 0 ? 0 : len;
   return p;
+}
+
+__device__ __forceinline__ ReqSpan span_of(const RaggedBatch& b, int r, int page_shift) {
+  return span_of(b, b.start[r], b.start[r + 1], b.kv_len[r], page_shift);
 }
 
 // The request of a token: the last r with start[r] <= tok (requests without
