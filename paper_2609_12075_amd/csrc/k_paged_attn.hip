@@ -237,14 +237,17 @@ __device__ __forceinline__ void empty_range(const PagedAttnArgs& a, const Item& 
 
 // ---------------------------------------------------------------- bf16 tiles in LDS
 // Tiles of K and V are key-major rows of HDP elements; the 16-byte piece c of
-// row r sits in slot c ^ swz(r), which keeps the reads of one piece of many
-// rows off each other's banks. They move global -> LDS with the direct loads
-// (lane l's 16 bytes at LDS base + 16 l).
+// row r sits in slot c ^ swz(r). LDS answers 256 bytes a cycle where they lie in
+// different banks: one piece of 16 rows (the scores' operand), 64 bytes of four
+// rows or 32 of eight (the transposing reads of 32 or 16 dims). The row's number
+// with its bits reversed spreads all three: the lowest bit moves a row by half
+// of the banks, the next by a quarter. (Unreversed, the transposing reads took
+// four times as long and LDS was busy for half of a long prompt's time.)
+// Tiles move global -> LDS with the direct loads (lane l's 16 bytes at LDS base + 16 l).
 template <int HDP>
 struct Lay {
-  static constexpr int CR = HDP / 8, ROWB = HDP * 2, RP = CR >= 16 ? 1 : 16 / CR, SWM = (CR >= 16 ? 16 : CR) - 1;
-  static constexpr int HX = CR >= 16 ? 2 : 1;  // eight rows further the swizzle differs by 4 HX pieces
-  __device__ static constexpr int swz(int r) { return (r / RP) & SWM; }
+  static constexpr int CR = HDP / 8, ROWB = HDP * 2, SW = CR >= 16 ? 0 : 1;   // (two rows of 64 dims are as wide as the banks)
+  __device__ static constexpr unsigned swz(unsigned r) { return __builtin_bitreverse32(r >> SW << (28 + SW)) & (15u >> SW); }
 };
 
 __device__ __forceinline__ unsigned lds_addr(const void* p) {
@@ -274,9 +277,9 @@ __device__ __forceinline__ bf16x4 read_tr(unsigned at) {
 }
 template <int HDP>
 __device__ __forceinline__ bf16x8 read_vt(unsigned at, int u, int off) {
-  const int hu = (u % 4) ^ Lay<HDP>::HX;
+  // (eight rows further the swizzle differs in its lowest bit)
   const bf16x4 l = read_tr((at ^ (u % 4 << 6)) + off + u / 4 * 256),
-               h = read_tr((at ^ (hu << 6)) + off + u / 4 * 256 + 8 * Lay<HDP>::ROWB);
+               h = read_tr((at ^ (u % 4 << 6) ^ 16) + off + u / 4 * 256 + 8 * Lay<HDP>::ROWB);
   return __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 // The lane's first byte for read_vt within a tile.
@@ -342,7 +345,7 @@ struct Mover {
   __device__ __forceinline__ Mover(const PagedAttnArgs& a, const Window& w, int wv) {
     const unsigned lane = threadIdx.x & 63;
     lrow = lane / Y::CR;
-    piece = ((lane % Y::CR) ^ (lrow / Y::RP)) << 4;
+    piece = ((lane % Y::CR) ^ Y::swz(lrow)) << 4;
     wave = wv;
     ts2 = (unsigned)(a.kv.tok_stride * 2);
     shift = a.kv.page_shift;
@@ -367,7 +370,7 @@ struct Mover {
       // cycles an instruction a loop of four is faster than 16 in a row)
 #pragma unroll 4
       for (int i = 0; i < N; ++i) {
-        const unsigned j = i * NWV + wave, off = row + (piece ^ (((j * RS / Y::RP) & Y::SWM) << 4));
+        const unsigned j = i * NWV + wave, off = row + (piece ^ (Y::swz(j * RS) << 4));
         const long b = (long)((unsigned long)(unsigned)__builtin_amdgcn_readlane(hi, i * RS) << 32 |
                               (unsigned)__builtin_amdgcn_readlane(lo, i * RS));
         dma16(kb + b, off, dst_k + j * 1024);
@@ -376,7 +379,7 @@ struct Mover {
     } else {
 #pragma unroll 1
       for (int i = 0; i < N; ++i) {
-        const unsigned j = i * NWV + wave, c = piece ^ (((j * RS / Y::RP) & Y::SWM) << 4);
+        const unsigned j = i * NWV + wave, c = piece ^ (Y::swz(j * RS) << 4);
         const int src = i * RS + lrow;
         const long b = __shfl(at, src) + c;
         const bool there = __shfl((int)ok, src) & (c < 2u * hd);
