@@ -13,6 +13,8 @@ from __future__ import annotations
 import ctypes
 from typing import Optional, Sequence
 
+import torch
+
 from . import vla
 
 EXPORTS = ["vla_kv_append", "vla_attention_workspace", "vla_paged_attention", "vla_shared_attention",
@@ -65,7 +67,6 @@ def _lib():
 
 
 def _dtype(t) -> int:
-    import torch
     if t.dtype == torch.bfloat16:
         return 1
     if t.dtype == torch.float32:
@@ -74,7 +75,6 @@ def _dtype(t) -> int:
 
 
 def _i32(t, name, shape, device):
-    import torch
     if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name} must be a contiguous int32 tensor {shape} on {device}, "
                          f"not {t.dtype} {tuple(t.shape)} on {t.device}")
@@ -96,8 +96,10 @@ class KVPool:
         self.k, self.v = k, v
         self.device, self.dtype = k.device, k.dtype
         n, h, p, d = k.shape
+        self.index, self.n_kv, self.head_dim = k.device.index, h, d
         self.c = KVPoolC(k.device.index, _dtype(k), h, d, p, n, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
                          k.stride(2))
+        self.ref = ctypes.byref(self.c)
 
 
 class Batch:
@@ -117,19 +119,28 @@ class Batch:
         self.c = RaggedC(n, n_tok, max_new, max_len, _i32(start, "start", (n + 1,), dev),
                          _i32(kv_len, "kv_len", (n,), dev), _i32(pages, "pages", (n, pages.shape[1]), dev),
                          pages.shape[1])
+        self.ref = ctypes.byref(self.c)
 
 
-def _rows(t, name, pool: KVPool, batch: Batch, heads: Optional[int]):
+# A call's kernels take a few microseconds where the batch is one token, so
+# the host's part is kept short: sizes compared as tuples, argument structures
+# built at once, the stream's handle without a stream object around it.
+def _rows(t, name, pool: KVPool, batch: Batch, heads: int):
     """Checks a token buffer [n_tok][heads][head_dim] and returns (address, token stride, head stride)."""
-    shape = t.shape
-    if len(shape) != 3 or shape[0] != batch.n_tok or shape[2] != pool.c.head_dim or (heads and shape[1] != heads):
-        raise ValueError(f"{name} must be [{batch.n_tok}, {heads or 'heads'}, {pool.c.head_dim}], not {tuple(shape)}")
+    if t.shape != (batch.n_tok, heads, pool.head_dim):
+        raise ValueError(f"{name} must be [{batch.n_tok}, {heads}, {pool.head_dim}], not {tuple(t.shape)}")
     if t.dtype != pool.dtype or t.device != pool.device:
         raise ValueError(f"{name} must be {pool.dtype} on {pool.device}, not {t.dtype} on {t.device}")
     ts, hs, ds = t.stride()
-    if ds != 1:
+    if ds != 1 and pool.head_dim > 1:
         raise ValueError(f"{name} must have contiguous rows")
     return t.data_ptr(), ts, hs
+
+
+def _heads(q):
+    if q.dim() != 3:
+        raise ValueError(f"q must be 3-d, not {tuple(q.shape)}")
+    return q.shape[1]
 
 
 def _same_device(pool: KVPool, batch: Batch):
@@ -139,9 +150,20 @@ def _same_device(pool: KVPool, batch: Batch):
 
 def _stream(pool: KVPool, stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream(pool.device).cuda_stream
+        return torch._C._cuda_getCurrentRawStream(pool.index)
     return vla._stream(stream)
+
+
+def _empty(shape, dtype, pool: KVPool, stream):
+    """A tensor for a call on `stream`, from that stream's own memory: what the
+    current stream's pool gives may still be in use by its earlier work."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=pool.device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=pool.device) if int(stream) else \
+            torch.cuda.default_stream(pool.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=pool.device)
 
 
 def append(pool: KVPool, batch: Batch, k, v, q=None, q_out=None, positions=None, sections: Sequence[int] = (),
@@ -151,66 +173,56 @@ def append(pool: KVPool, batch: Batch, k, v, q=None, q_out=None, positions=None,
     (empty: no rotation); positions int32 [n_tok][len(sections)] or None (one
     axis: the tokens' places). Returns q_out (allocated unless given)."""
     _same_device(pool, batch)
-    n_kv = pool.c.n_kv
-    a = AppendArgsC()
-    a.k, a.k_tok_stride, a.k_head_stride = _rows(k, "k", pool, batch, n_kv)
-    a.v, a.v_tok_stride, a.v_head_stride = _rows(v, "v", pool, batch, n_kv)
-    if q is not None:
-        a.n_q = q.shape[1] if q.dim() == 3 else 0
-        a.q, a.q_tok_stride, a.q_head_stride = _rows(q, "q", pool, batch, None)
-        if q_out is None:
-            import torch
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        a.q_out, a.qo_tok_stride, a.qo_head_stride = _rows(q_out, "q_out", pool, batch, a.n_q)
-    if len(sections) > 3:
+    n = len(sections)
+    if n > 3:
         raise ValueError("at most three axes")
-    a.n_axes = len(sections)
-    for i, s in enumerate(sections):
-        a.sections[i] = s
-    if positions is not None:
-        a.positions = _i32(positions, "positions", (batch.n_tok, len(sections)), pool.device)
-    a.rope_base = rope_base
-    vla._check(_lib().vla_kv_append(ctypes.byref(pool.c), ctypes.byref(batch.c), ctypes.byref(a), _stream(pool, stream)))
+    n_q, qr, qo = 0, (None, 0, 0), (None, 0, 0)
+    if q is not None:
+        n_q = _heads(q)
+        qr = _rows(q, "q", pool, batch, n_q)
+        if q_out is None:
+            q_out = _empty(q.shape, q.dtype, pool, stream)
+        qo = _rows(q_out, "q_out", pool, batch, n_q)
+    kp, kt, kh = _rows(k, "k", pool, batch, pool.n_kv)
+    vp, vt, vh = _rows(v, "v", pool, batch, pool.n_kv)
+    pos = None if positions is None else _i32(positions, "positions", (batch.n_tok, n), pool.device)
+    a = AppendArgsC(kp, vp, kt, kh, vt, vh, n_q, qr[0], qo[0], qr[1], qr[2], qo[1], qo[2], n, tuple(sections), pos,
+                    rope_base)
+    vla._check(_lib().vla_kv_append(pool.ref, batch.ref, ctypes.byref(a), _stream(pool, stream)))
     return q_out
 
 
 def _attend(pool, batch, q, shared_len, out, lse, scale, cap, causal, window, prefix, ws, stream):
-    import torch
     _same_device(pool, batch)
-    L = _lib()
-    a = AttentionArgsC()
-    a.q, a.q_tok_stride, a.q_head_stride = _rows(q, "q", pool, batch, None)
-    a.n_q = q.shape[1]
+    L = _L or _lib()
+    n_q = _heads(q)
+    qp, qt, qh = _rows(q, "q", pool, batch, n_q)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    a.o, a.o_tok_stride, a.o_head_stride = _rows(out, "out", pool, batch, a.n_q)
+        out = _empty(q.shape, q.dtype, pool, stream)
+    op, ot, oh = _rows(out, "out", pool, batch, n_q)
+    lp = None
     if lse is not None:
-        if lse.dtype != torch.float32 or tuple(lse.shape) != (batch.n_tok, a.n_q) or not lse.is_contiguous() \
+        if lse.dtype != torch.float32 or lse.shape != (batch.n_tok, n_q) or not lse.is_contiguous() \
                 or lse.device != pool.device:
-            raise ValueError(f"lse must be a contiguous float32 tensor [{batch.n_tok}, {a.n_q}] on {pool.device}")
-        a.lse = lse.data_ptr()
-    a.scale, a.cap, a.causal, a.window = scale, cap, int(bool(causal)), window
-    if prefix is not None:
-        a.prefix = _i32(prefix, "prefix", (batch.n_req,), pool.device)
-    p, b, r = ctypes.byref(pool.c), ctypes.byref(batch.c), ctypes.byref(a)
+            raise ValueError(f"lse must be a contiguous float32 tensor [{batch.n_tok}, {n_q}] on {pool.device}")
+        lp = lse.data_ptr()
+    pf = None if prefix is None else _i32(prefix, "prefix", (batch.n_req,), pool.device)
+    a = AttentionArgsC(qp, op, qt, qh, ot, oh, lp, n_q, scale, cap, 1 if causal else 0, window, pf, None, 0)
+    r = ctypes.byref(a)
     if ws is None:
         need = ctypes.c_size_t()
-        vla._check(L.vla_attention_workspace(p, b, r, shared_len or 0, ctypes.byref(need)))
+        vla._check(L.vla_attention_workspace(pool.ref, batch.ref, r, shared_len or 0, ctypes.byref(need)))
         if need.value:
-            # the allocator hands it out again only behind the calls of the stream it was allocated on
-            ws = torch.empty(need.value, dtype=torch.uint8, device=pool.device)
-            if stream is not None:
-                ws.record_stream(stream if hasattr(stream, "cuda_stream") else
-                                 torch.cuda.ExternalStream(int(stream), device=pool.device))
+            ws = _empty((need.value,), torch.uint8, pool, stream)
+    elif ws.device != pool.device or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous tensor on {pool.device}")
     if ws is not None:
-        if ws.device != pool.device or not ws.is_contiguous():
-            raise ValueError(f"ws must be a contiguous tensor on {pool.device}")
         a.ws, a.ws_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
     s = _stream(pool, stream)
     if shared_len is None:
-        vla._check(L.vla_paged_attention(p, b, r, s))
+        vla._check(L.vla_paged_attention(pool.ref, batch.ref, r, s))
     else:
-        vla._check(L.vla_shared_attention(p, b, r, shared_len, s))
+        vla._check(L.vla_shared_attention(pool.ref, batch.ref, r, shared_len, s))
     return out
 
 
@@ -236,6 +248,5 @@ def workspace_bytes(pool: KVPool, batch: Batch, n_q: int, shared_len: int = 0, c
     """vla_attention_workspace: scratch bytes of such an attention (host only)."""
     a = AttentionArgsC(n_q=n_q, causal=int(bool(causal)), window=window)
     need = ctypes.c_size_t()
-    vla._check(_lib().vla_attention_workspace(ctypes.byref(pool.c), ctypes.byref(batch.c), ctypes.byref(a), shared_len,
-                                              ctypes.byref(need)))
+    vla._check(_lib().vla_attention_workspace(pool.ref, batch.ref, ctypes.byref(a), shared_len, ctypes.byref(need)))
     return need.value
