@@ -589,37 +589,38 @@ __device__ __forceinline__ void put_stats(const PagedAttnArgs& a, const Item& it
 }
 
 // ---------------------------------------------------------------- bf16, waves split the rows
-// 128 rows a block, 32 a wave; KS groups of four waves take every KS-th key
-// tile, whose four waves load it together, through a ring of two rounds. (64
-// keys a tile; 32 at head dim 256.) Two groups where the blocks are few: their
-// results meet in LDS.
-template <int HDP, int KS>
+// 32 rows a wave, 32 NWR a block. KS groups of NWR waves take every KS-th SUB
+// key tiles, which a group's waves load together, through a ring of two rounds.
+// (64 keys a tile; 32 at head dim 256.) Eight waves of rows and two tiles a
+// round where there are rows enough: half the loads and round overhead of four.
+// Two groups of four where the blocks are few: their results meet in LDS.
+template <int HDP, int KS, int NWR>
 struct RowsShared {
-  static constexpr int KT = HDP == 256 ? 32 : 64, RING = 2 * KS * 2 * KT * Lay<HDP>::ROWB;
+  static constexpr int KT = HDP == 256 ? 32 : 64, SUB = NWR / 4, RING = 2 * KS * SUB * 2 * KT * Lay<HDP>::ROWB;
   static constexpr int MERGE = KS > 1 ? 256 * HDP * 2 : 0;       // half of each group's outputs
   __attribute__((aligned(1024))) char mem[RING > MERGE ? RING : MERGE];
   Window win;
-  float stats[KS][128][2];
+  float stats[KS][KS > 1 ? 128 : 1][2];
 };
 
-template <int HDP, bool CAP, int KS, bool FLAT>
-__device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP, KS>& sh, int L, int range) {
+template <int HDP, bool CAP, int KS, int NWR, bool FLAT>
+__device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP, KS, NWR>& sh, int L, int range) {
   using Y = Lay<HDP>;
-  constexpr int KT = RowsShared<HDP, KS>::KT, NS = KT / 32, NC = HDP / 16, ND = HDP / 32;
-  constexpr int TILE = KT * Y::ROWB, ROUND = KS * 2 * TILE;
+  constexpr int KT = RowsShared<HDP, KS, NWR>::KT, SUB = RowsShared<HDP, KS, NWR>::SUB, NS = KT / 32, NC = HDP / 16, ND = HDP / 32;
+  constexpr int TILE = SUB * KT * Y::ROWB, ROUND = KS * 2 * TILE, BR = 32 * NWR, RTL = KS * SUB;   // RTL: tiles of a round
   char* smem = sh.mem;
   Window& win = sh.win;
   auto& stats = sh.stats;
   touch(a);
   Item it;
-  if (!find_item<128, KT, KS, FLAT>(a, L, range, it)) return;
+  if (!find_item<BR, KT, RTL, FLAT>(a, L, range, it)) return;
   const bool direct = a.direct && it.ntiles <= a.chunk;
   if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
-    if (!direct) empty_range<128>(a, it);
+    if (!direct) empty_range<BR>(a, it);
     return;
   }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int kg = wave >> 2, wr = wave & 3;
+  const int kg = wave / NWR, wr = wave % NWR;
   const int lq = lane & 31, h = lane >> 5, hd = a.kv.hd, shift = a.kv.page_shift;
   const int wrow = it.row0 + wr * 32;
   const bool active = wrow < it.nrows;
@@ -644,18 +645,18 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
   const unsigned ring = lds_addr(smem);
   int w0 = 0;
   bool holes = false;
-  Mover<HDP, KT, 4> mv(a, win, wr);
+  Mover<HDP, SUB * KT, NWR> mv(a, win, wr);
   auto issue = [&](int p) {                    // round p
-    const int u = it.ubeg + p * KS + kg;
+    const int u = it.ubeg + p * RTL + kg * SUB;
     if (u >= it.uend) return;
     const unsigned dst = ring + (p & 1) * ROUND + kg * 2 * TILE;
     mv.rows(first_key(u), w0, it.klim);
     mv.template load<true>(kb, vb, dst, dst + TILE);
   };
-  const int nrounds = (it.uend - it.ubeg + KS - 1) / KS;
+  const int nrounds = (it.uend - it.ubeg + RTL - 1) / RTL;
   if (nrounds > 0) {
     w0 = first_key(it.ubeg) >> shift;
-    holes = fill_window<256 * KS>(a, it, win, w0);
+    holes = fill_window<64 * NWR * KS>(a, it, win, w0);
     issue(0);
   }
   hold<NC, 16>(8 * h, hd, hd == HDP, qf);
@@ -667,16 +668,18 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
     // this round has landed, and every wave is done with the round before
     asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (p + 1 < nrounds) {
-      const int n0 = first_key(it.ubeg + (p + 1) * KS), e0 = n0 >> shift, e1 = (min(n0 + KS * KT, it.klim) - 1) >> shift;
+      const int n0 = first_key(it.ubeg + (p + 1) * RTL), e0 = n0 >> shift, e1 = (min(n0 + RTL * KT, it.klim) - 1) >> shift;
       if (e0 < w0 || e1 >= w0 + PW) {          // (block-uniform; the barrier was the window's last use)
         w0 = e0;
-        holes |= fill_window<256 * KS>(a, it, win, w0);
+        holes |= fill_window<64 * NWR * KS>(a, it, win, w0);
       }
       issue(p + 1);
     }
-    const int u = it.ubeg + p * KS + kg, k0 = first_key(u);
+#pragma unroll 1
+    for (int sub = 0; sub < SUB; ++sub) {
+    const int u = it.ubeg + p * RTL + kg * SUB + sub, k0 = first_key(u);
     if (!active || u >= it.uend || tile_unseen(wl, k0, k0 + KT)) continue;
-    unsigned kt = ring + (p & 1) * ROUND + kg * 2 * TILE + ka, vt = kt - ka + TILE + va;
+    unsigned kt = ring + (p & 1) * ROUND + kg * 2 * TILE + sub * (KT * Y::ROWB) + ka, vt = kt - ka + TILE + va;
     asm volatile("" : "+v"(kt), "+v"(vt));
     // fragments are requested well ahead of their products (LDS answers after
     // a few of these): all keys' first, two groups of the values' before the
@@ -722,9 +725,11 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
       if constexpr (AHEAD)
         if (c + 2 < KT / 16) values(c + 2);
     }
+    }
   }
   s.l = sum_x32(s.l);
   if (active) {
+    // (SUB is 1 where there are two groups)
     const int mine = it.uend - it.ubeg - kg;
     repair<HDP, CAP>(a, it, s, qf, w.lim, sl2, c1, c2, mine > 0 ? (mine + KS - 1) / KS : 0, KT,
                      [&](int n) { return first_key(it.ubeg + n * KS + kg); });
@@ -1074,11 +1079,14 @@ __device__ __forceinline__ void keys_body(const PagedAttnArgs& a, KeysShared<HDP
 // context, of that (all rows in one sequence of tiles, the grid's first
 // blocks) and KIND2 of what follows it: the two do not wait for each other.
 template <int HDP, bool CAP, int KIND>
-__global__ void __launch_bounds__(KIND == PAGED_ROWS2 ? 512 : 256, KIND == PAGED_KEYS2 && HDP == 256 ? 1 : 2)
+__global__ void __launch_bounds__(KIND == PAGED_ROWS8 || KIND == PAGED_ROWS2 ? 512 : 256, KIND == PAGED_KEYS2 && HDP == 256 ? 1 : 2)
     paged_kernel(PagedAttnArgs a) {
-  if constexpr (KIND == PAGED_ROWS || KIND == PAGED_ROWS2) {
-    __shared__ RowsShared<HDP, KIND == PAGED_ROWS2 ? 2 : 1> sh;
-    rows_body<HDP, CAP, KIND == PAGED_ROWS2 ? 2 : 1, false>(a, sh, blockIdx.x, blockIdx.y);
+  if constexpr (KIND == PAGED_ROWS8) {
+    __shared__ RowsShared<HDP, 1, 8> sh;
+    rows_body<HDP, CAP, 1, 8, false>(a, sh, blockIdx.x, blockIdx.y);
+  } else if constexpr (KIND == PAGED_ROWS2) {
+    __shared__ RowsShared<HDP, 2, 4> sh;
+    rows_body<HDP, CAP, 2, 4, false>(a, sh, blockIdx.x, blockIdx.y);
   } else {
     __shared__ KeysShared<HDP, KIND == PAGED_KEYS2 ? 2 : 1> sh;
     keys_body<HDP, KIND == PAGED_KEYS2 ? 2 : 1, CAP, false>(a, sh, blockIdx.x, blockIdx.y);
@@ -1089,7 +1097,7 @@ template <int HDP, bool CAP, int KIND, int KIND2>
 __global__ void __launch_bounds__(256, (KIND == PAGED_KEYS2 || KIND2 == PAGED_KEYS2) && HDP == 256 ? 1 : 2)
     paged_pair_kernel(PagedAttnArgs a, PagedAttnArgs b) {
   union Shared {
-    RowsShared<HDP, 1> rows;
+    RowsShared<HDP, 1, 4> rows;
     KeysShared<HDP, 1> keys;
     KeysShared<HDP, KIND == PAGED_KEYS2 || KIND2 == PAGED_KEYS2 ? 2 : 1> keys2;
   };
@@ -1100,7 +1108,7 @@ __global__ void __launch_bounds__(256, (KIND == PAGED_KEYS2 || KIND2 == PAGED_KE
   if (L < na) {
     const int range = div_by(L, per_a, a.mul_blocks);
     L -= range * per_a;
-    if constexpr (KIND == PAGED_ROWS) rows_body<HDP, CAP, 1, true>(a, sh.rows, L, range);
+    if constexpr (KIND == PAGED_ROWS) rows_body<HDP, CAP, 1, 4, true>(a, sh.rows, L, range);
     else if constexpr (KIND == PAGED_KEYS) keys_body<HDP, 1, CAP, true>(a, sh.keys, L, range);
     else keys_body<HDP, 2, CAP, true>(a, sh.keys2, L, range);
   } else {
@@ -1108,7 +1116,7 @@ __global__ void __launch_bounds__(256, (KIND == PAGED_KEYS2 || KIND2 == PAGED_KE
     L -= na;
     const int range = div_by(L, per_b, b.mul_blocks);
     L -= range * per_b;
-    if constexpr (KIND2 == PAGED_ROWS) rows_body<HDP, CAP, 1, false>(b, sh.rows, L, range);
+    if constexpr (KIND2 == PAGED_ROWS) rows_body<HDP, CAP, 1, 4, false>(b, sh.rows, L, range);
     else if constexpr (KIND2 == PAGED_KEYS) keys_body<HDP, 1, CAP, false>(b, sh.keys, L, range);
     else keys_body<HDP, 2, CAP, false>(b, sh.keys2, L, range);
   }
@@ -1376,12 +1384,12 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a) {
 // ---------------------------------------------------------------- host
 // Rows of a tile, keys of a key tile and key tiles of a round of kernel k at
 // padded head dim hdp.
-static int tile_rows(int k) { return k == PAGED_KEYS2 ? 32 : k == PAGED_ROWS || k == PAGED_ROWS2 ? 128 : 16; }
+static int tile_rows(int k) { return k == PAGED_KEYS2 ? 32 : k == PAGED_ROWS8 ? 256 : k == PAGED_ROWS || k == PAGED_ROWS2 ? 128 : 16; }
 static int tile_keys(int k, int hdp) {
   const int wide = hdp == 256 ? 1 : 2;
   return k == PAGED_F32 ? 16 : k == PAGED_KEYS || k == PAGED_KEYS2 ? 16 * wide : 32 * wide;
 }
-static int round_tiles(int k) { return k == PAGED_KEYS || k == PAGED_KEYS2 ? 4 : k == PAGED_ROWS2 ? 2 : 1; }
+static int round_tiles(int k) { return k == PAGED_KEYS || k == PAGED_KEYS2 ? 4 : k == PAGED_ROWS2 || k == PAGED_ROWS8 ? 2 : 1; }
 
 // Key ranges of a part: the count that minimises the time of a simple model:
 // waves of resident blocks times (start + rounds of tiles), and where a row has
@@ -1390,11 +1398,11 @@ static void cut(PagedPart& p, int hdp, int hd, int keys, int n_kv, long rows) {
   const int kt = tile_keys(p.kernel, hdp), unit = round_tiles(p.kernel);
   const long total = std::max(1, (keys + kt * unit - 1) / (kt * unit));      // rounds
   const long blocks = (long)p.tiles * n_kv;
-  const long resident = p.kernel == PAGED_ROWS2 || hdp == 256 ? 256 : 512;
+  const long resident = p.kernel == PAGED_ROWS2 || p.kernel == PAGED_ROWS8 || hdp == 256 ? 256 : 512;
   const double start = 3.0, merge = 3.0, bytes = 4.0 * kt * unit * hd;
   double best = 1e30;
   long best_per = total;
-  const long most = p.kernel != PAGED_ROWS && p.kernel != PAGED_ROWS2 ? 256 : std::max<long>(1, resident / blocks);
+  const long most = p.kernel != PAGED_ROWS && p.kernel != PAGED_ROWS2 && p.kernel != PAGED_ROWS8 ? 256 : std::max<long>(1, resident / blocks);
   for (long s = 1; s <= std::min(total, most); ++s) {
     const long per = (total + s - 1) / s, n = (total + per - 1) / per;
     if (n != s) continue;
@@ -1420,9 +1428,17 @@ PagedPlan paged_plan(const PagedAttnArgs& a, int et) {
       const long r = flat ? all : rows_req;
       q.kernel = r <= 16 ? PAGED_KEYS : r <= 32 ? PAGED_KEYS2 : PAGED_ROWS;
     }
-    const int br = tile_rows(q.kernel);
+    int br = tile_rows(q.kernel);
     q.tiles = (int)(flat ? std::max<long>(1, (all + br - 1) / br) : rows_req <= br ? a.bt.n_req : all / br + a.bt.n_req);
-    if (q.kernel == PAGED_ROWS && a.shared_len == 0 && (long)q.tiles * a.kv.n_kv <= 256) q.kernel = PAGED_ROWS2;
+    if (q.kernel == PAGED_ROWS && a.shared_len == 0) {
+      if ((long)q.tiles * a.kv.n_kv <= 256) {
+        q.kernel = PAGED_ROWS2;
+      } else {
+        q.kernel = PAGED_ROWS8;
+        br = tile_rows(q.kernel);
+        q.tiles = (int)(rows_req <= br ? a.bt.n_req : all / br + a.bt.n_req);
+      }
+    }
     cut(q, p.hdp, a.kv.hd, keys, a.kv.n_kv, (long)a.bt.n_tok * a.n_q);
     return q;
   };
@@ -1450,7 +1466,7 @@ static void launch_one(const PagedAttnArgs& a, int kernel, bool flat, hipStream_
   const dim3 grid((unsigned)a.tiles * a.kv.n_kv, a.ranges);
   if (kernel == PAGED_KEYS) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_KEYS>), grid, dim3(256), 0, s, a);
   else if (kernel == PAGED_KEYS2) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_KEYS2>), grid, dim3(256), 0, s, a);
-  else if (kernel == PAGED_ROWS) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_ROWS>), grid, dim3(256), 0, s, a);
+  else if (kernel == PAGED_ROWS8) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_ROWS8>), grid, dim3(512), 0, s, a);
   else if (kernel == PAGED_ROWS2) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_ROWS2>), grid, dim3(512), 0, s, a);
   else if (flat) hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP, true>), grid, dim3(512), 0, s, a);
   else hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP, false>), grid, dim3(512), 0, s, a);
