@@ -15,6 +15,8 @@
 // element by element. Ranges of one tile of rows go to different blocks where
 // the rows alone would not fill the chip, and are merged by a second kernel.
 #include <algorithm>
+#include <cmath>
+#include <initializer_list>
 #include <type_traits>
 
 #include "paged.h"
@@ -694,6 +696,9 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
         for (int c = 0; c < NC; ++c) kf[st][c] = read_k(kt, c, st * 32 * Y::ROWB);
       __builtin_amdgcn_sched_barrier(0);
     }
+    // (at head dim 256 the products go first: five capped prompts of 866 tokens 48.4 -> 47.0 us; at 64 and 128,
+    // where the softmax is the longer part, the other way round)
+    if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int st = 0; st < NS; ++st) {
 #pragma unroll
@@ -704,6 +709,7 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
         sc[st] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[AHEAD ? st : 0][c], qf[c], sc[st], 0, 0, 0);
       }
     }
+    if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(0);
     bf16x8 vf[2][ND];
     auto values = [&](int c) {
 #pragma unroll
@@ -715,6 +721,7 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
       __builtin_amdgcn_sched_barrier(0);
     }
     softmax_tile<HDP, NS, CAP>(s, sc, sl2, c1, c2, !holes && tile_full(wl, k0, k0 + KT), w.lim, k0, a, it, holes);
+    if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int c = 0; c < KT / 16; ++c) {
       const bf16x8 pf = weights_of(sc[c / 2], c % 2);
@@ -725,6 +732,7 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
       if constexpr (AHEAD)
         if (c + 2 < KT / 16) values(c + 2);
     }
+    if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(0);
     }
   }
   s.l = sum_x32(s.l);
@@ -785,7 +793,7 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
 }
 
 // ---------------------------------------------------------------- bf16, waves split the keys
-// 16 RT rows a block; wave w takes every fourth tile of 32 keys (16 at head dim 256) into a K and a
+// 16 rows a block; wave w takes every fourth tile of 32 keys (16 at head dim 256) into a K and a
 // V slot of its own and waits for its own loads only: no barrier in the loop,
 // and a slot is loaded again as soon as its fragments are in registers. The
 // waves' (max, sum, output) meet in LDS at the end. For single tokens, whose
@@ -812,19 +820,19 @@ __device__ __forceinline__ f32x4 pv_mma(bf16x4 v, bf16x4 p, f32x4 o) {
   return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(v4s, v), __builtin_bit_cast(v4s, p), o, 0, 0, 0);
 }
 
-template <int HDP, int RT>
+template <int HDP>
 struct KeysShared {
   static constexpr int KT = HDP == 256 ? 16 : 32, NW = 4;
-  static constexpr int SLOTS = NW * 2 * KT * Lay<HDP>::ROWB, MERGE = NW * RT * HDP / 16 * 1024;
+  static constexpr int SLOTS = NW * 2 * KT * Lay<HDP>::ROWB, MERGE = NW * HDP / 16 * 1024;
   __attribute__((aligned(1024))) char mem[SLOTS > MERGE ? SLOTS : MERGE];
   Window win;
-  float stats[NW][16 * RT][2];
+  float stats[NW][16][2];
 };
 
-template <int HDP, int RT, bool CAP, bool FLAT>
-__device__ __forceinline__ void keys_body(const PagedAttnArgs& a, KeysShared<HDP, RT>& sh, int L, int range) {
+template <int HDP, bool CAP, bool FLAT>
+__device__ __forceinline__ void keys_body(const PagedAttnArgs& a, KeysShared<HDP>& sh, int L, int range) {
   using Y = Lay<HDP>;
-  constexpr int KT = KeysShared<HDP, RT>::KT, NST = KT / 16, NW = 4, NC = HDP / 32, ND = HDP / 16;
+  constexpr int KT = KeysShared<HDP>::KT, NST = KT / 16, NW = 4, NC = HDP / 32, ND = HDP / 16;
   constexpr int TILE = KT * Y::ROWB, LK = TILE / 1024;
   char* smem = sh.mem;
   Window& win = sh.win;
@@ -832,36 +840,27 @@ __device__ __forceinline__ void keys_body(const PagedAttnArgs& a, KeysShared<HDP
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), shift = a.kv.page_shift;
   touch(a);
   // the page numbers that the range needs if no window moves it: requested with the batch's lengths
-  const int guess = (a.klo + range * a.chunk * KT) >> shift;
+  // (where a request is one tile of rows, the block knows which)
+  const int guess = FLAT || a.bt.max_new * a.G <= 16 ? (a.klo + range * a.chunk * KT) >> shift : -1;
   int guessed = 0;
-  if (a.bt.pages_stride > 0) {
+  if (guess >= 0 && a.bt.pages_stride > 0) {
     const int tile = div_by(L, a.kv.n_kv, a.mul_kv), r = FLAT ? 0 : (a.causal ? a.tiles - 1 - tile : tile);
     guessed = a.bt.pages[(long)r * a.bt.pages_stride + min(guess + tid, a.bt.pages_stride - 1)];
   }
   Item it;
-  if (!find_item<16 * RT, KT, NW, FLAT>(a, L, range, it)) return;
+  if (!find_item<16, KT, NW, FLAT>(a, L, range, it)) return;
   const bool direct = a.direct && it.ntiles <= a.chunk;
   if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
-    if (!direct) empty_range<16 * RT>(a, it);
+    if (!direct) empty_range<16>(a, it);
     return;
   }
   const int lq = lane & 15, grp = lane >> 4, hd = a.kv.hd;
-  Row w[RT];
-  WaveLimits wl;
-  bf16x8 qf[RT][NC];
-  f32x4 o[RT][ND];
-  float m[RT], l[RT];
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    w[t] = row_of<FLAT>(a, it, it.row0 + t * 16 + lq);
-    const WaveLimits x = wave_limits<16, FLAT>(a, w[t].lim);
-    wl = t == 0 ? x : WaveLimits{min(wl.pre0, x.pre0), max(wl.pre1, x.pre1), min(wl.lo0, x.lo0), max(wl.lo1, x.lo1),
-                                 min(wl.hi0, x.hi0), max(wl.hi1, x.hi1)};
-    const bf16* qp = reinterpret_cast<const bf16*>(a.q) + (long)w[t].tok * a.q_ts + (long)w[t].head * a.q_hs;
-    load_q<NC, 32>(qp, 8 * grp, hd, qf[t]);
-    m[t] = -INFINITY;
-    l[t] = 0.f;
-  }
+  const Row w = row_of<FLAT>(a, it, it.row0 + lq);
+  const WaveLimits wl = wave_limits<16, FLAT>(a, w.lim);
+  bf16x8 qf[NC];
+  f32x4 o[ND];
+  float m = -INFINITY, l = 0.f;
+  load_q<NC, 32>(reinterpret_cast<const bf16*>(a.q) + (long)w.tok * a.q_ts + (long)w.head * a.q_hs, 8 * grp, hd, qf);
   const float sl2 = a.scale * LOG2E, c1 = CAP ? 2.f * sl2 / a.cap : 0.f, c2 = a.cap * LOG2E;
   auto first_key = [&](int u) { return a.klo + (u < it.n1 ? u : u - it.n1 + it.t2) * KT; };
   const char *kb = reinterpret_cast<const char*>(a.kv.k), *vb = reinterpret_cast<const char*>(a.kv.v);
@@ -883,11 +882,8 @@ __device__ __forceinline__ void keys_body(const PagedAttnArgs& a, KeysShared<HDP
   float zero = 0.f;
   asm volatile("" : "+v"(zero));
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-#pragma unroll
-    for (int u = 0; u < ND; ++u) o[t][u] = f32x4{zero, zero, zero, zero};
-    hold<NC, 32>(8 * grp, hd, hd == HDP, qf[t]);
-  }
+  for (int u = 0; u < ND; ++u) o[u] = f32x4{zero, zero, zero, zero};
+  hold<NC, 32>(8 * grp, hd, hd == HDP, qf);
   const unsigned ka = slot_k + lq * Y::ROWB + ((grp ^ Y::swz(lq)) << 4);
   const int vr = 4 * grp + (lq >> 2);
   const unsigned va = slot_v + vr * Y::ROWB + ((((lq & 3) >> 1) ^ Y::swz(vr)) << 4) + ((lq & 1) << 3);
@@ -923,52 +919,49 @@ __device__ __forceinline__ void keys_body(const PagedAttnArgs& a, KeysShared<HDP
     }
     const bool full = !holes && tile_full(wl, k0, k0 + KT);
     typedef __attribute__((ext_vector_type(4 * NST))) __bf16 frag;   // the keys of a lane
-    frag pf[RT];
+    frag pf;
+    f32x4 sc[NST];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      f32x4 sc[NST];
+    for (int st = 0; st < NST; ++st) {
+      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;         // two chains
 #pragma unroll
-      for (int st = 0; st < NST; ++st) {
-        f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;         // two chains
-#pragma unroll
-        for (int c = 0; c < NC; c += 2) {
-          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[st][c], qf[t][c], s0, 0, 0, 0);
-          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[st][c + 1], qf[t][c + 1], s1, 0, 0, 0);
-        }
-        sc[st] = s0 + s1;
+      for (int c = 0; c < NC; c += 2) {
+        s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[st][c], qf[c], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[st][c + 1], qf[c + 1], s1, 0, 0, 0);
       }
-      float mx = -INFINITY;
+      sc[st] = s0 + s1;
+    }
+    float mx = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 4 * NST; ++i) {
-        float x = sc[i / 4][i % 4];
-        x = CAP ? capped(x, c1, c2) : x * sl2;
-        if (!full) {
-          const int j = k0 + i / 4 * 16 + 4 * grp + i % 4;
-          if (!sees(w[t].lim, j)) x = -INFINITY;
-          if (holes && (unsigned)it.pages[min(j, it.klim - 1) >> shift] >= (unsigned)a.kv.n_pages) x = -INFINITY;
-        }
-        sc[i / 4][i % 4] = x;
-        mx = vmax(mx, x);
+    for (int i = 0; i < 4 * NST; ++i) {
+      float x = sc[i / 4][i % 4];
+      x = CAP ? capped(x, c1, c2) : x * sl2;
+      if (!full) {
+        const int j = k0 + i / 4 * 16 + 4 * grp + i % 4;
+        if (!sees(w.lim, j)) x = -INFINITY;
+        if (holes && (unsigned)it.pages[min(j, it.klim - 1) >> shift] >= (unsigned)a.kv.n_pages) x = -INFINITY;
       }
-      mx = max_x32(max_x16(mx));
-      // (the reference follows only a growth of 2^8, as in softmax_tile)
-      if (__ballot(mx > m[t] + 8.f)) {
-        const float mn = vmax(m[t], mx), alpha = __builtin_amdgcn_exp2f(m[t] - (mn == -INFINITY ? 0.f : mn));
-        const bool some = __ballot(m[t] != -INFINITY) != 0;      // (else there is nothing yet to rescale)
-        m[t] = mn;
-        l[t] *= alpha;
-        if (some) {
+      sc[i / 4][i % 4] = x;
+      mx = vmax(mx, x);
+    }
+    mx = max_x32(max_x16(mx));
+    // (the reference follows only a growth of 2^8, as in softmax_tile)
+    if (__ballot(mx > m + 8.f)) {
+      const float mn = vmax(m, mx), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.f : mn));
+      const bool some = __ballot(m != -INFINITY) != 0;      // (else there is nothing yet to rescale)
+      m = mn;
+      l *= alpha;
+      if (some) {
 #pragma unroll
-          for (int u2 = 0; u2 < ND; ++u2) o[t][u2] *= alpha;
-        }
+        for (int u2 = 0; u2 < ND; ++u2) o[u2] *= alpha;
       }
-      const float ref = m[t] == -INFINITY ? 0.f : m[t];
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-      for (int i = 0; i < 4 * NST; ++i) {
-        const float x = __builtin_amdgcn_exp2f(sc[i / 4][i % 4] - ref);
-        l[t] += x;
-        pf[t][i] = (bf16)x;
-      }
+    for (int i = 0; i < 4 * NST; ++i) {
+      const float x = __builtin_amdgcn_exp2f(sc[i / 4][i % 4] - ref);
+      l += x;
+      pf[i] = (bf16)x;
     }
     // the values have landed once only the next keys' loads are pending
     if (next) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LK) : "memory");
@@ -984,54 +977,46 @@ __device__ __forceinline__ void keys_body(const PagedAttnArgs& a, KeysShared<HDP
     __builtin_amdgcn_sched_barrier(0);
     if (next) mv.template load<false>(vb, nullptr, slot_v, 0);
 #pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int u2 = 0; u2 < ND; ++u2) o[t][u2] = pv_mma(vf[u2], pf[t], o[t][u2]);
+    for (int u2 = 0; u2 < ND; ++u2) o[u2] = pv_mma(vf[u2], pf, o[u2]);
   }
   float z = 0.f;
+  l = sum_x32(sum_x16(l));
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    l[t] = sum_x32(sum_x16(l[t]));
+  for (int u = 0; u < ND; ++u)
 #pragma unroll
-    for (int u = 0; u < ND; ++u)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) z = __builtin_fmaf(o[t][u][e], 0.f, z);
-  }
+    for (int e = 0; e < 4; ++e) z = __builtin_fmaf(o[u][e], 0.f, z);
   // rows with an output that is not finite: again, key by key (as `repair`)
   if (__ballot(z != z) != 0) {
+    const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const float ref = m[t] == -INFINITY ? 0.f : m[t];
-#pragma unroll
-      for (int u = 0; u < ND; ++u) o[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < ND; ++u) o[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-      for (int u = it.ubeg + wave; u < it.uend; u += NW) {
-        const int k0 = first_key(u);
+    for (int u = it.ubeg + wave; u < it.uend; u += NW) {
+      const int k0 = first_key(u);
 #pragma unroll 1
-        for (int j = k0; j < min(k0 + KT, it.klim); ++j) {
-          const bool vis = sees(w[t].lim, j);
-          if (__ballot(vis) == 0) continue;
-          const long off = page_offset(a, it.pages[j >> shift], it.g);
-          if (off < 0) continue;
-          const long at = off + (long)(j & ((1 << shift) - 1)) * a.kv.tok_stride;
-          float d = 0.f;
+      for (int j = k0; j < min(k0 + KT, it.klim); ++j) {
+        const bool vis = sees(w.lim, j);
+        if (__ballot(vis) == 0) continue;
+        const long off = page_offset(a, it.pages[j >> shift], it.g);
+        if (off < 0) continue;
+        const long at = off + (long)(j & ((1 << shift) - 1)) * a.kv.tok_stride;
+        float d = 0.f;
 #pragma unroll
-          for (int c = 0; c < NC; ++c)
-            if (32 * c + 8 * grp < hd) {
-              const bf16x8 x = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const bf16*>(a.kv.k) + at + 32 * c + 8 * grp);
+        for (int c = 0; c < NC; ++c)
+          if (32 * c + 8 * grp < hd) {
+            const bf16x8 x = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const bf16*>(a.kv.k) + at + 32 * c + 8 * grp);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) d = __builtin_fmaf((float)x[e], (float)qf[t][c][e], d);
-            }
-          d = sum_x32(sum_x16(d));
-          const float pj = __builtin_amdgcn_exp2f((CAP ? capped(d, c1, c2) : d * sl2) - ref);
+            for (int e = 0; e < 8; ++e) d = __builtin_fmaf((float)x[e], (float)qf[c][e], d);
+          }
+        d = sum_x32(sum_x16(d));
+        const float pj = __builtin_amdgcn_exp2f((CAP ? capped(d, c1, c2) : d * sl2) - ref);
 #pragma unroll
-          for (int u2 = 0; u2 < ND; ++u2)
-            if (vis && 16 * u2 + 4 * grp < hd) {
-              const bf16x4 x = *reinterpret_cast<const bf16x4*>(reinterpret_cast<const bf16*>(a.kv.v) + at + 16 * u2 + 4 * grp);
+        for (int u2 = 0; u2 < ND; ++u2)
+          if (vis && 16 * u2 + 4 * grp < hd) {
+            const bf16x4 x = *reinterpret_cast<const bf16x4*>(reinterpret_cast<const bf16*>(a.kv.v) + at + 16 * u2 + 4 * grp);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[t][u2][e] = __builtin_fmaf(pj, (float)x[e], o[t][u2][e]);
-            }
-        }
+            for (int e = 0; e < 4; ++e) o[u2][e] = __builtin_fmaf(pj, (float)x[e], o[u2][e]);
+          }
       }
     }
   }
@@ -1039,48 +1024,37 @@ __device__ __forceinline__ void keys_body(const PagedAttnArgs& a, KeysShared<HDP
   __syncthreads();
   f32x4* mo = reinterpret_cast<f32x4*>(smem);
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-#pragma unroll
-    for (int u = 0; u < ND; ++u) mo[((wave * RT + t) * ND + u) * 64 + lane] = o[t][u];
-    if (grp == 0) {
-      stats[wave][t * 16 + lq][0] = m[t];
-      stats[wave][t * 16 + lq][1] = l[t];
-    }
+  for (int u = 0; u < ND; ++u) mo[(wave * ND + u) * 64 + lane] = o[u];
+  if (grp == 0) {
+    stats[wave][lq][0] = m;
+    stats[wave][lq][1] = l;
   }
   __syncthreads();
+  float mm = -INFINITY, ll = 0.f, wt[NW];
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int row = t * 16 + lq;
-    float mm = -INFINITY, ll = 0.f, wt[NW];
+  for (int q = 0; q < NW; ++q) mm = vmax(mm, stats[q][lq][0]);
 #pragma unroll
-    for (int q = 0; q < NW; ++q) mm = vmax(mm, stats[q][row][0]);
-#pragma unroll
-    for (int q = 0; q < NW; ++q) {
-      // (a wave without keys weighs nothing)
-      wt[q] = stats[q][row][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stats[q][row][0] - mm);
-      ll += stats[q][row][1] * wt[q];
-    }
-    if (it.row0 + row >= it.nrows) continue;
-    const float inv = inverse(ll);
-    // (a wave, or a row of it, without keys has stored zeros)
-    const f32x4* mine = mo + (t * ND + wave * (ND / NW)) * 64 + lane;
-    put<HDP, ND / NW>(a, it, w[t], direct, inv, [&](int i) { return 16 * (wave * (ND / NW) + i) + 4 * grp; }, [&](int i) {
-      f32x4 acc = mine[i * 64] * wt[0];
-#pragma unroll
-      for (int q = 1; q < NW; ++q) acc += mine[(q * RT * ND + i) * 64] * wt[q];
-      return acc;
-    });
-    if (wave == 0 && grp == 0) put_stats(a, it, w[t], direct, mm, ll);
+  for (int q = 0; q < NW; ++q) {
+    // (a wave without keys weighs nothing)
+    wt[q] = stats[q][lq][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stats[q][lq][0] - mm);
+    ll += stats[q][lq][1] * wt[q];
   }
+  if (it.row0 + lq >= it.nrows) return;
+  const float inv = inverse(ll);
+  // (a wave, or a row of it, without keys has stored zeros)
+  const f32x4* mine = mo + wave * (ND / NW) * 64 + lane;
+  put<HDP, ND / NW>(a, it, w, direct, inv, [&](int i) { return 16 * (wave * (ND / NW) + i) + 4 * grp; }, [&](int i) {
+    f32x4 acc = mine[i * 64] * wt[0];
+#pragma unroll
+    for (int q = 1; q < NW; ++q) acc += mine[(q * ND + i) * 64] * wt[q];
+    return acc;
+  });
+  if (wave == 0 && grp == 0) put_stats(a, it, w, direct, mm, ll);
 }
 
 // ---------------------------------------------------------------- bf16 kernels
-// KIND: PagedKernel of the whole attention, or, for a batch with a common
-// context, of that (all rows in one sequence of tiles, the grid's first
-// blocks) and KIND2 of what follows it: the two do not wait for each other.
 template <int HDP, bool CAP, int KIND>
-__global__ void __launch_bounds__(KIND == PAGED_ROWS8 || KIND == PAGED_ROWS2 ? 512 : 256, KIND == PAGED_KEYS2 && HDP == 256 ? 1 : 2)
-    paged_kernel(PagedAttnArgs a) {
+__global__ void __launch_bounds__(KIND == PAGED_KEYS ? 256 : 512, 2) paged_kernel(PagedAttnArgs a) {
   if constexpr (KIND == PAGED_ROWS8) {
     __shared__ RowsShared<HDP, 1, 8> sh;
     rows_body<HDP, CAP, 1, 8, false>(a, sh, blockIdx.x, blockIdx.y);
@@ -1088,20 +1062,21 @@ __global__ void __launch_bounds__(KIND == PAGED_ROWS8 || KIND == PAGED_ROWS2 ? 5
     __shared__ RowsShared<HDP, 2, 4> sh;
     rows_body<HDP, CAP, 2, 4, false>(a, sh, blockIdx.x, blockIdx.y);
   } else {
-    __shared__ KeysShared<HDP, KIND == PAGED_KEYS2 ? 2 : 1> sh;
-    keys_body<HDP, KIND == PAGED_KEYS2 ? 2 : 1, CAP, false>(a, sh, blockIdx.x, blockIdx.y);
+    __shared__ KeysShared<HDP> sh;
+    keys_body<HDP, CAP, false>(a, sh, blockIdx.x, blockIdx.y);
   }
 }
 
-template <int HDP, bool CAP, int KIND, int KIND2>
-__global__ void __launch_bounds__(256, (KIND == PAGED_KEYS2 || KIND2 == PAGED_KEYS2) && HDP == 256 ? 1 : 2)
-    paged_pair_kernel(PagedAttnArgs a, PagedAttnArgs b) {
+// A batch with a common context: that by KIND (all rows in one sequence of
+// tiles, the grid's first blocks), what follows it in tiles of 16 rows: the two
+// do not wait for each other.
+template <int HDP, bool CAP, int KIND>
+__global__ void __launch_bounds__(256, 2) paged_pair_kernel(PagedAttnArgs a, PagedAttnArgs b) {
   union Shared {
     RowsShared<HDP, 1, 4> rows;
-    KeysShared<HDP, 1> keys;
-    KeysShared<HDP, KIND == PAGED_KEYS2 || KIND2 == PAGED_KEYS2 ? 2 : 1> keys2;
+    KeysShared<HDP> keys;
   };
-  __shared__ __attribute__((aligned(1024))) char mem[sizeof(Shared)];
+  __shared__ __attribute__((aligned(1024))) char mem[KIND == PAGED_ROWS ? sizeof(Shared) : sizeof(KeysShared<HDP>)];
   Shared& sh = *reinterpret_cast<Shared*>(mem);
   const int per_a = a.tiles * a.kv.n_kv, na = per_a * a.ranges;
   int L = blockIdx.x;
@@ -1109,16 +1084,13 @@ __global__ void __launch_bounds__(256, (KIND == PAGED_KEYS2 || KIND2 == PAGED_KE
     const int range = div_by(L, per_a, a.mul_blocks);
     L -= range * per_a;
     if constexpr (KIND == PAGED_ROWS) rows_body<HDP, CAP, 1, 4, true>(a, sh.rows, L, range);
-    else if constexpr (KIND == PAGED_KEYS) keys_body<HDP, 1, CAP, true>(a, sh.keys, L, range);
-    else keys_body<HDP, 2, CAP, true>(a, sh.keys2, L, range);
+    else keys_body<HDP, CAP, true>(a, sh.keys, L, range);
   } else {
     const int per_b = b.tiles * b.kv.n_kv;
     L -= na;
     const int range = div_by(L, per_b, b.mul_blocks);
     L -= range * per_b;
-    if constexpr (KIND2 == PAGED_ROWS) rows_body<HDP, CAP, 1, 4, false>(b, sh.rows, L, range);
-    else if constexpr (KIND2 == PAGED_KEYS) keys_body<HDP, 1, CAP, false>(b, sh.keys, L, range);
-    else keys_body<HDP, 2, CAP, false>(b, sh.keys2, L, range);
+    keys_body<HDP, CAP, false>(b, sh.keys, L, range);
   }
 }
 
@@ -1384,75 +1356,113 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a) {
 // ---------------------------------------------------------------- host
 // Rows of a tile, keys of a key tile and key tiles of a round of kernel k at
 // padded head dim hdp.
-static int tile_rows(int k) { return k == PAGED_KEYS2 ? 32 : k == PAGED_ROWS8 ? 256 : k == PAGED_ROWS || k == PAGED_ROWS2 ? 128 : 16; }
+static int tile_rows(int k) { return k == PAGED_ROWS8 ? 256 : k == PAGED_ROWS || k == PAGED_ROWS2 ? 128 : 16; }
 static int tile_keys(int k, int hdp) {
   const int wide = hdp == 256 ? 1 : 2;
-  return k == PAGED_F32 ? 16 : k == PAGED_KEYS || k == PAGED_KEYS2 ? 16 * wide : 32 * wide;
+  return k == PAGED_F32 ? 16 : k == PAGED_KEYS ? 16 * wide : 32 * wide;
 }
-static int round_tiles(int k) { return k == PAGED_KEYS || k == PAGED_KEYS2 ? 4 : k == PAGED_ROWS2 || k == PAGED_ROWS8 ? 2 : 1; }
+static int round_tiles(int k) { return k == PAGED_KEYS ? 4 : k == PAGED_ROWS2 || k == PAGED_ROWS8 ? 2 : k == PAGED_F32 ? 2 : 1; }
 
-// Key ranges of a part: the count that minimises the time of a simple model:
-// waves of resident blocks times (start + rounds of tiles), and where a row has
-// several ranges the merge's launch and the bytes of the outputs it reads.
-static void cut(PagedPart& p, int hdp, int hd, int keys, int n_kv, long rows) {
-  const int kt = tile_keys(p.kernel, hdp), unit = round_tiles(p.kernel);
-  const long total = std::max(1, (keys + kt * unit - 1) / (kt * unit));      // rounds
-  const long blocks = (long)p.tiles * n_kv;
-  const long resident = p.kernel == PAGED_ROWS2 || p.kernel == PAGED_ROWS8 || hdp == 256 ? 256 : 512;
-  const double start = 3.0, merge = 3.0, bytes = 4.0 * kt * unit * hd;
+// How long a part would take with kernel p.kernel (us) by a simple model, and
+// the number of key ranges that makes it least: the blocks' start, as many
+// rounds of tiles at a time as blocks are resident, each at a round's latency,
+// a block's bytes at what one CU takes in, or all bytes at the memory's rate
+// (requests' keys differ) or the L2's; a part of a last block's rounds, as
+// lengths differ and it runs alone; and, where a row has several ranges, the merge's
+// launch and their outputs. Starts and rounds are measured; the model
+// need only be right where the kernels' times differ much. (One request's token
+// over 881 keys of 8 heads of 256: ranges of 64 keys 10.5 us, 128 11.9, 256
+// 13.8. 64 tokens over up to 8101 keys of 8 heads of 128: one range 272 us, four
+// 262, eight 259, sixteen 270. Twelve prompts of 64 over 864 keys of 8 heads of
+// 256: in tiles of 16 rows and two ranges 24.1 us, of 128 and one range 39.6,
+// four 29.7; five of 866, capped: 110 against 48. One prompt of 4000 of 15 heads of 64:
+// tiles of 16 rows 97 us, 128 55, 256 77; of 8191 of 32 heads of 128: 128 rows 636, 256 580.)
+struct PartShape {
+  int hdp, hd, keys, seen, n_kv, n_req;        // seen: keys that a tile of rows sees at most
+  long rows;
+  double share;                                // of `seen` that the tiles see on average
+  bool cap, beside;
+};
+
+static double cut(PagedPart& p, const PartShape& q) {
+  const int w = q.hdp == 64 ? 0 : q.hdp == 128 ? 1 : 2, kt = tile_keys(p.kernel, q.hdp), unit = round_tiles(p.kernel);
+  const int es = p.kernel == PAGED_F32 ? 4 : 2;
+  // by PagedKernel and padded head dim
+  static const double START[5][3] = {{4, 5, 5}, {5, 7.5, 12}, {4, 4, 4}, {5, 7.5, 12}, {5, 7.5, 12}};
+  static const double ROUND[5][3] = {{1, 1, 1.3}, {1, 1.2, 1.7}, {1, 1, 1}, {1.55, 1.8, 1.9}, {2.3, 3.1, 3.1}};
+  static const int RESIDENT[5][3] = {{1024, 512, 512}, {512, 512, 256}, {512, 512, 512}, {256, 256, 256}, {256, 256, 256}};
+  const long full = std::max(1, (q.keys + kt * unit - 1) / (kt * unit));     // rounds of all keys
+  const long total = std::max(1, (q.seen + kt * unit - 1) / (kt * unit));
+  const long blocks = (long)p.tiles * q.n_kv, resident = RESIDENT[p.kernel][w];
+  const bool small = p.kernel == PAGED_KEYS;   // (two blocks and more a CU slow each other down)
+  const double bytes = 2.0 * es * kt * unit * q.hd, differ = std::min(1.0, (double)q.n_req / p.tiles);
   double best = 1e30;
-  long best_per = total;
-  const long most = p.kernel != PAGED_ROWS && p.kernel != PAGED_ROWS2 && p.kernel != PAGED_ROWS8 ? 256 : std::max<long>(1, resident / blocks);
+  long best_per = full;
+  // (the parts of a batch with a common context run side by side)
+  const long most = std::min<long>(256, std::max<long>(1, (q.beside ? 512 : 4 * resident) / blocks));
   for (long s = 1; s <= std::min(total, most); ++s) {
-    const long per = (total + s - 1) / s, n = (total + per - 1) / per;
-    if (n != s) continue;
-    const double on = (double)std::min(blocks * s, resident);
-    const double round = std::max(1.0, bytes * on / 5e6);                     // us
-    const double t = (double)((blocks * s + resident - 1) / resident) * (start + per * round) +
-                     (s > 1 ? merge + rows * (double)s * hd * 8 / 4e6 : 0.0);
-    if (t < best) { best = t; best_per = per; }
+    const long per = (total + s - 1) / s, n = s > 1 ? (full + per - 1) / per : 1;
+    if ((total + per - 1) / per != s) continue;
+    const double on = (double)std::min(blocks * s, resident), per_cu = blocks * s / 256.0, passes = blocks * s / (double)resident;
+    const double uneven = per_cu > 1.0 && per_cu <= resident / 256 ? std::ceil(per_cu) / per_cu : 1.0;
+    const double rounds = p.kernel == PAGED_F32 ? (per + 3) / 4 : per;         // (eight waves, a tile each)
+    const double slow = (small && passes > 1.0 ? 1.25 : 1.0) * (small && q.cap ? 1.3 : 1.0);
+    const double busy = std::max(rounds * ROUND[p.kernel][w] * slow,
+                                 per * bytes * std::max({1e-5, on * differ * uneven / 5e6, on / 15e6}));
+    const double t = START[p.kernel][w] + std::ceil(passes) +
+                     busy * (q.share < 0.95 ? std::max(1.0, passes * q.share + 0.3) : std::ceil(passes)) +
+                     (small || p.kernel == PAGED_F32 ? 0.5 * rounds : 0.0) +
+                     (n > 1 ? 4.0 + q.rows * (double)n * q.hd * 8 / 2e6 : 0.0);
+    if (t < best) { best = t; best_per = s > 1 ? per : full; }
   }
-  best_per = std::max<long>(best_per, (total + 65534) / 65535);               // (the grid's second extent)
+  best_per = std::max<long>(best_per, (full + 65534) / 65535);                // (the grid's second extent)
   p.chunk = (int)(best_per * unit);
-  p.ranges = (int)((total + best_per - 1) / best_per);
+  p.ranges = (int)((full + best_per - 1) / best_per);
+  return best;
 }
 
 PagedPlan paged_plan(const PagedAttnArgs& a, int et) {
   PagedPlan p{};
   p.hdp = a.kv.hd <= 64 ? 64 : a.kv.hd <= 128 ? 128 : 256;
-  const long all = (long)a.bt.n_tok * a.G;
-  auto part = [&](long rows_req, bool flat, int keys) {
-    PagedPart q{};
-    q.kernel = et == ET_F32 ? PAGED_F32 : PAGED_ROWS;
-    if (et != ET_F32) {
-      const long r = flat ? all : rows_req;
-      q.kernel = r <= 16 ? PAGED_KEYS : r <= 32 ? PAGED_KEYS2 : PAGED_ROWS;
-    }
-    int br = tile_rows(q.kernel);
+  const long all = (long)a.bt.n_tok * a.G, rows_req = (long)a.bt.max_new * a.G;
+  // a part by kernel k: flat: the rows of the batch in one sequence of tiles
+  auto part = [&](int k, bool flat, int keys, PagedPart& q) {
+    const int br = tile_rows(k);
+    q.kernel = k;
     q.tiles = (int)(flat ? std::max<long>(1, (all + br - 1) / br) : rows_req <= br ? a.bt.n_req : all / br + a.bt.n_req);
-    if (q.kernel == PAGED_ROWS && a.shared_len == 0) {
-      if ((long)q.tiles * a.kv.n_kv <= 256) {
-        q.kernel = PAGED_ROWS2;
-      } else {
-        q.kernel = PAGED_ROWS8;
-        br = tile_rows(q.kernel);
-        q.tiles = (int)(rows_req <= br ? a.bt.n_req : all / br + a.bt.n_req);
-      }
-    }
-    cut(q, p.hdp, a.kv.hd, keys, a.kv.n_kv, (long)a.bt.n_tok * a.n_q);
-    return q;
+    const int seen = a.causal && a.window && !flat ? (int)std::min<long>(keys, (long)a.window + br / a.G + 1) : keys;
+    const double share = a.causal && !a.window && !a.prefix && !flat && keys > 0 ? 1.0 - 0.5 * std::min(a.bt.max_new, keys) / keys : 1.0;
+    return cut(q, PartShape{p.hdp, a.kv.hd, keys, seen, a.kv.n_kv, flat ? 1 : a.bt.n_req, (long)a.bt.n_tok * a.n_q, share, a.cap > 0.f, a.shared_len > 0});
   };
-  const long rows_req = (long)a.bt.max_new * a.G;
-  if (a.shared_len > 0) {
-    p.n_parts = 2;
-    p.part[0] = part(rows_req, true, a.shared_len);
-    p.part[1] = part(rows_req, false, a.bt.max_len - a.shared_len);
-    p.slots = p.part[0].ranges + p.part[1].ranges;
+  auto least = [&](std::initializer_list<int> kernels, bool flat, int keys) {
+    PagedPart best{};
+    double t = 1e30;
+    for (int k : kernels) {
+      PagedPart q{};
+      const double tk = part(k, flat, keys, q);
+      if (tk < t) { t = tk; best = q; }
+    }
+    return best;
+  };
+  const int rest = a.bt.max_len - a.shared_len;
+  p.n_parts = a.shared_len > 0 ? 2 : 1;
+  if (et == ET_F32) {
+    if (a.shared_len > 0) p.part[0] = least({PAGED_F32}, true, a.shared_len);
+    p.part[p.n_parts - 1] = least({PAGED_F32}, false, rest);
+  } else if (a.shared_len > 0) {
+    // Up to 32 tiles of 16 rows (128 at head dim 256, where a block of 128 rows takes long to begin and end) the
+    // common context goes in those, beyond in tiles of 128: 16 rows x 2 x 8 heads of 128 over 4096 keys 15.7 and 16.9 us,
+    // x 6 x 8 21.5 and 20.8, x 16 x 2 16.3 and 18.6; of 256 x 32 over 832 13.9 and 20.5, x 128 over 2048 31.5 and
+    // 36.5, x 192 over 4096 65 and 43. What follows is a few keys of many requests: tiles of 16 (or as fast).
+    const long tiles16 = (all + 15) / 16 * a.kv.n_kv;
+    p.part[0] = least({tiles16 <= (p.hdp == 256 ? 128 : 32) ? PAGED_KEYS : PAGED_ROWS}, true, a.shared_len);
+    p.part[1] = least({PAGED_KEYS}, false, rest);
+  } else if (rows_req <= 16) {
+    p.part[0] = least({PAGED_KEYS}, false, rest);
   } else {
-    p.n_parts = 1;
-    p.part[0] = part(rows_req, false, a.bt.max_len);
-    p.slots = p.part[0].ranges;
+    p.part[0] = least({PAGED_KEYS, PAGED_ROWS2, PAGED_ROWS8}, false, rest);
   }
+  for (int i = 0; i < p.n_parts; ++i) p.slots += p.part[i].ranges;
   return p;
 }
 
@@ -1465,37 +1475,24 @@ template <int HDP, bool CAP>
 static void launch_one(const PagedAttnArgs& a, int kernel, bool flat, hipStream_t s) {
   const dim3 grid((unsigned)a.tiles * a.kv.n_kv, a.ranges);
   if (kernel == PAGED_KEYS) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_KEYS>), grid, dim3(256), 0, s, a);
-  else if (kernel == PAGED_KEYS2) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_KEYS2>), grid, dim3(256), 0, s, a);
   else if (kernel == PAGED_ROWS8) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_ROWS8>), grid, dim3(512), 0, s, a);
   else if (kernel == PAGED_ROWS2) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_ROWS2>), grid, dim3(512), 0, s, a);
   else if (flat) hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP, true>), grid, dim3(512), 0, s, a);
   else hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP, false>), grid, dim3(512), 0, s, a);
 }
 
-// The two parts of a batch with a common context. (a request's rows are some
-// of the batch's, so the second part has no more rows a tile than the first)
+// The two parts of a batch with a common context.
 template <int HDP, bool CAP>
-static void launch_pair(const PagedAttnArgs& a, const PagedAttnArgs& b, int ka, int kb, hipStream_t s) {
+static void launch_pair(const PagedAttnArgs& a, const PagedAttnArgs& b, int ka, hipStream_t s) {
   const dim3 grid((unsigned)(a.tiles * a.kv.n_kv * a.ranges + b.tiles * b.kv.n_kv * b.ranges));
-#define PAIR(A, B) hipLaunchKernelGGL((paged_pair_kernel<HDP, CAP, A, B>), grid, dim3(256), 0, s, a, b)
-  if (ka == PAGED_ROWS) {
-    if (kb == PAGED_ROWS) PAIR(PAGED_ROWS, PAGED_ROWS);
-    else if (kb == PAGED_KEYS2) PAIR(PAGED_ROWS, PAGED_KEYS2);
-    else PAIR(PAGED_ROWS, PAGED_KEYS);
-  } else if (ka == PAGED_KEYS2) {
-    if (kb == PAGED_KEYS2) PAIR(PAGED_KEYS2, PAGED_KEYS2);
-    else PAIR(PAGED_KEYS2, PAGED_KEYS);
-  } else {
-    PAIR(PAGED_KEYS, PAGED_KEYS);
-  }
-#undef PAIR
+  if (ka == PAGED_ROWS) hipLaunchKernelGGL((paged_pair_kernel<HDP, CAP, PAGED_ROWS>), grid, dim3(256), 0, s, a, b);
+  else hipLaunchKernelGGL((paged_pair_kernel<HDP, CAP, PAGED_KEYS>), grid, dim3(256), 0, s, a, b);
 }
 
 template <int HDP, bool CAP>
 static void launch_parts(const PagedAttnArgs (&a)[2], const PagedPlan& p, hipStream_t s) {
-  const int ka = p.part[0].kernel, kb = p.part[1].kernel;
-  if (p.n_parts == 2 && ka != PAGED_F32) {
-    launch_pair<HDP, CAP>(a[0], a[1], ka, kb, s);
+  if (p.n_parts == 2 && p.part[0].kernel != PAGED_F32) {
+    launch_pair<HDP, CAP>(a[0], a[1], p.part[0].kernel, s);
     return;
   }
   for (int i = 0; i < p.n_parts; ++i) launch_one<HDP, CAP>(a[i], p.part[i].kernel, p.n_parts == 2 && i == 0, s);

@@ -52,11 +52,12 @@ struct PagedAttnArgs {
 };
 
 // How an attention is computed. PAGED_KEYS: a block owns 16 rows (token, query
-// head of the group), its waves split the keys; PAGED_KEYS2: 32 rows; PAGED_ROWS: its waves split 128
-// rows; PAGED_ROWS2: so do two groups of waves, which split the keys; PAGED_ROWS8: eight waves split 256 rows; PAGED_F32:
-// fp32, 16 rows, waves split the keys. One part over the cache, or two: the common context (all rows
+// head of the group), its waves split the keys; PAGED_ROWS: its waves split 128
+// rows; PAGED_ROWS2: so do two groups of waves, which split the keys;
+// PAGED_ROWS8: eight waves split 256 rows; PAGED_F32: fp32, 16 rows, waves
+// split the keys. One part over the cache, or two: the common context (all rows
 // of the batch in one sequence of tiles) and what follows it.
-enum PagedKernel { PAGED_KEYS = 0, PAGED_ROWS = 1, PAGED_F32 = 2, PAGED_ROWS2 = 3, PAGED_KEYS2 = 4, PAGED_ROWS8 = 5 };
+enum PagedKernel { PAGED_KEYS = 0, PAGED_ROWS = 1, PAGED_F32 = 2, PAGED_ROWS2 = 3, PAGED_ROWS8 = 4 };
 struct PagedPart { int kernel, tiles, chunk, ranges; };
 struct PagedPlan { int n_parts, hdp, slots; PagedPart part[2]; };
 PagedPlan paged_plan(const PagedAttnArgs& a, int et);
