@@ -1388,9 +1388,9 @@ static double cut(PagedPart& p, const PartShape& q) {
   const int w = q.hdp == 64 ? 0 : q.hdp == 128 ? 1 : 2, kt = tile_keys(p.kernel, q.hdp), unit = round_tiles(p.kernel);
   const int es = p.kernel == PAGED_F32 ? 4 : 2;
   // by PagedKernel and padded head dim
-  static const double START[5][3] = {{4, 5, 5}, {5, 7.5, 12}, {4, 4, 4}, {5, 7.5, 12}, {5, 7.5, 12}};
-  static const double ROUND[5][3] = {{1, 1, 1.3}, {1, 1.2, 1.7}, {1, 1, 1}, {1.55, 1.8, 1.9}, {2.3, 3.1, 3.1}};
-  static const int RESIDENT[5][3] = {{1024, 512, 512}, {512, 512, 256}, {512, 512, 512}, {256, 256, 256}, {256, 256, 256}};
+  static const double START[5][3] = {{4, 5, 5}, {5, 7.5, 12}, {4, 4, 4}, {5, 7.5, 12}, {0, 5.5, 0}};
+  static const double ROUND[5][3] = {{1, 1, 1.3}, {1, 1.2, 1.7}, {1, 1, 1}, {1.55, 1.8, 1.9}, {0, 3.1, 0}};
+  static const int RESIDENT[5][3] = {{1024, 512, 512}, {512, 512, 256}, {512, 512, 512}, {256, 256, 256}, {0, 256, 0}};
   const long full = std::max(1, (q.keys + kt * unit - 1) / (kt * unit));     // rounds of all keys
   const long total = std::max(1, (q.seen + kt * unit - 1) / (kt * unit));
   const long blocks = (long)p.tiles * q.n_kv, resident = RESIDENT[p.kernel][w];
@@ -1459,10 +1459,22 @@ PagedPlan paged_plan(const PagedAttnArgs& a, int et) {
     p.part[1] = least({PAGED_KEYS}, false, rest);
   } else if (rows_req <= 16) {
     p.part[0] = least({PAGED_KEYS}, false, rest);
-  } else {
+  } else if (p.hdp == 128) {
+    // (256 rows a block pay off here only: two prompts of 4000 of 32 heads of 128 303 -> 270 us, four of 1500 of 8 heads of
+    // 64 23 -> 34, two of 1500 of 16 heads of 256 63 -> 91)
     p.part[0] = least({PAGED_KEYS, PAGED_ROWS2, PAGED_ROWS8}, false, rest);
+  } else {
+    p.part[0] = least({PAGED_KEYS, PAGED_ROWS2}, false, rest);
   }
-  for (int i = 0; i < p.n_parts; ++i) p.slots += p.part[i].ranges;
+  // (a launch has less than 2^32 threads in x; a merge's rows have up to 256 each)
+  long blocks = 0;
+  for (int i = 0; i < p.n_parts; ++i) {
+    const PagedPart& q = p.part[i];
+    p.slots += q.ranges;
+    blocks += (long)q.tiles * a.kv.n_kv * (p.n_parts == 2 ? q.ranges : 1);
+  }
+  VLA_REQUIRE(blocks < 1 << 23 && (p.slots == 1 || (long)a.bt.n_tok * a.n_q < 1 << 24),
+              "too many rows for one call: " + std::to_string(a.bt.n_tok) + " tokens of " + std::to_string(a.n_q) + " heads");
   return p;
 }
 
@@ -1475,7 +1487,7 @@ template <int HDP, bool CAP>
 static void launch_one(const PagedAttnArgs& a, int kernel, bool flat, hipStream_t s) {
   const dim3 grid((unsigned)a.tiles * a.kv.n_kv, a.ranges);
   if (kernel == PAGED_KEYS) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_KEYS>), grid, dim3(256), 0, s, a);
-  else if (kernel == PAGED_ROWS8) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_ROWS8>), grid, dim3(512), 0, s, a);
+  else if (HDP == 128 && kernel == PAGED_ROWS8) hipLaunchKernelGGL((paged_kernel<HDP, CAP, HDP == 128 ? PAGED_ROWS8 : PAGED_KEYS>), grid, dim3(512), 0, s, a);
   else if (kernel == PAGED_ROWS2) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_ROWS2>), grid, dim3(512), 0, s, a);
   else if (flat) hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP, true>), grid, dim3(512), 0, s, a);
   else hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP, false>), grid, dim3(512), 0, s, a);

@@ -250,3 +250,18 @@ def workspace_bytes(pool: KVPool, batch: Batch, n_q: int, shared_len: int = 0, c
     need = ctypes.c_size_t()
     vla._check(_lib().vla_attention_workspace(pool.ref, batch.ref, ctypes.byref(a), shared_len, ctypes.byref(need)))
     return need.value
+
+
+def attention_plan(n_req: int, n_tok: int, max_new: int, max_len: int, n_q: int, n_kv: int, head_dim: int, page: int = 16,
+                   shared_len: int = 0, bf16: bool = True, causal: bool = True, window: int = 0, prefix: bool = False,
+                   cap: float = 0.0) -> dict:
+    """vla_debug_paged_plan: how an attention of such sizes is launched (host
+    only): the padded head dim and, a part each, (kernel, row tiles, key tiles a
+    range, ranges)."""
+    pool = KVPoolC(0, 1 if bf16 else 0, n_kv, head_dim, page, 1, None, None, 0, page * head_dim, head_dim)
+    batch = RaggedC(n_req, n_tok, max_new, max_len, None, None, None, -(-max_len // page))
+    a = AttentionArgsC(n_q=n_q, causal=1 if causal else 0, window=window, prefix=64 if prefix else None, cap=cap)
+    plan = (_ci * 9)()
+    vla._check(_lib().vla_debug_paged_plan(ctypes.byref(pool), ctypes.byref(batch), ctypes.byref(a), shared_len, plan))
+    parts = [tuple(plan[1 + 4 * i:5 + 4 * i]) for i in range(2) if plan[1 + 4 * i] >= 0]
+    return {"hdp": plan[0], "parts": [(("keys", "rows", "f32", "rows2", "rows8")[p[0]],) + p[1:] for p in parts]}

@@ -207,3 +207,13 @@ def test_append_reference_rotates_like_complex_numbers():
         assert torch.allclose(qo[t, :, :8], z.real) and torch.allclose(qo[t, :, 8:16], z.imag)
         assert torch.equal(qo[t, :, 16:], c.q[t, :, 16:].double())
     assert torch.equal(vp[c.table[1][0], 0, 2], v[4, 0].double())
+
+
+def test_plans_without_a_gpu_and_the_bounds_of_one_call():
+    """The launch plan is host only; rows that no launch holds are refused before anything is enqueued."""
+    p = paged.attention_plan(1, 1, 1, 881, 8, 1, 256, page=64)
+    assert p["hdp"] == 256 and p["parts"][0][0] == "keys" and p["parts"][0][3] > 1
+    assert [k[0] for k in paged.attention_plan(8, 8, 1, 900, 4, 4, 64, shared_len=512, bf16=False)["parts"]] == ["f32"] * 2
+    for kw in (dict(bf16=True), dict(bf16=False)):
+        with pytest.raises(vla.VlaError, match="too many rows"):
+            paged.attention_plan(65535, 65535, 1, 64, 4096, 4096, 64, **kw)
