@@ -152,7 +152,7 @@ vla_status vla_shared_attention(const vla_kv_pool* pool, const vla_ragged* batch
  * padded to, then for the whole attention, or for the common context and what
  * follows it: kernel (0 tiles of 16 rows, waves split the keys, 1 tiles of 128
  * rows, waves split them, 2 fp32, 3 as 1 with two groups of waves that split the
- * keys, 4 tiles of 256 rows, -1 no such part), row tiles, key tiles a range,
+ * keys, 4 tiles of 256 rows, 5 as 2 with tiles of 64 or 32 rows, -1 no such part), row tiles, key tiles a range,
  * ranges.
  */
 vla_status vla_debug_paged_plan(const vla_kv_pool* pool, const vla_ragged* batch, const vla_attention_args* args,

@@ -1095,37 +1095,78 @@ __global__ void __launch_bounds__(256, 2) paged_pair_kernel(PagedAttnArgs a, Pag
 }
 
 // ---------------------------------------------------------------- fp32
-// 16 rows a block, eight waves split the tiles of 16 keys; both products on
+// 16 RT rows a block, eight waves split the tiles of 16 keys; both products on
 // v_mfma_f32_16x16x4_f32 with operands straight from global memory. A tile's
-// page numbers are requested while the tile before is computed.
-template <int HDP, bool CAP, bool FLAT>
-__global__ void __launch_bounds__(512) paged_f32_kernel(PagedAttnArgs a) {
-  constexpr int NW = 8, KT = 16, NC = HDP / 16, REC = HDP / 4 + 4;
-  __shared__ __attribute__((aligned(16))) float mg[NW / 2][64 * REC];
+// page numbers are requested while the tile before is computed. RT is 1 for few
+// rows; for prompts 4 at head dim 64 and 2 at 128 (what the registers hold), which
+// read the keys and values that much less often.
+template <int HDP>
+struct F32Shared {
+  static constexpr int REC = HDP / 4 + 4;
+  __attribute__((aligned(16))) float mg[4][64 * REC];
+};
+static constexpr int f32_row_tiles(int hdp) { return hdp == 64 ? 4 : hdp == 128 ? 2 : 1; }
+
+template <int HDP, bool CAP, int RT, bool FLAT>
+__device__ __forceinline__ void f32_body(const PagedAttnArgs& a, F32Shared<HDP>& sh, int L, int range) {
+  constexpr int NW = 8, KT = 16, NC = HDP / 16, REC = F32Shared<HDP>::REC;
+  auto& mg = sh.mg;
   Item it;
-  if (!find_item<16, KT, 1, FLAT>(a, blockIdx.x, blockIdx.y, it)) return;
+  if (!find_item<16 * RT, KT, 1, FLAT>(a, L, range, it)) return;
   const bool direct = a.direct && it.ntiles <= a.chunk;
   if (it.ubeg >= it.uend && !(direct && it.ubeg == 0)) {
-    if (!direct) empty_range<16>(a, it);
+    if (!direct) empty_range<16 * RT>(a, it);
     return;
   }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 15, lk = lane >> 4, hd = a.kv.hd, shift = a.kv.page_shift, smask = (1 << shift) - 1;
-  const Row w = row_of<FLAT>(a, it, it.row0 + lr);
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  const float* qp = reinterpret_cast<const float*>(a.q) + (long)w.tok * a.q_ts + (long)w.head * a.q_hs;
-  f32x4 qf[NC], o[NC];
+  Row w[RT];
+  f32x4 qf[RT][NC], o[RT][NC];
+  float m[RT], l[RT];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    qf[c] = c * 16 + lk * 4 < hd ? *reinterpret_cast<const f32x4*>(qp + c * 16 + lk * 4) : zero;
-    o[c] = zero;
+  for (int t = 0; t < RT; ++t) {
+    w[t] = row_of<FLAT>(a, it, it.row0 + t * 16 + lr);
+    const float* qp = reinterpret_cast<const float*>(a.q) + (long)w[t].tok * a.q_ts + (long)w[t].head * a.q_hs;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      qf[t][c] = c * 16 + lk * 4 < hd ? *reinterpret_cast<const f32x4*>(qp + c * 16 + lk * 4) : zero;
+      o[t][c] = zero;
+    }
+    m[t] = -INFINITY;
+    l[t] = 0.f;
   }
-  float m = -INFINITY, l = 0.f;
   auto first_key = [&](int u) { return a.klo + (u < it.n1 ? u : u - it.n1 + it.t2) * KT; };
   auto page_at = [&](int j) { return it.pages[min(j, it.klim - 1) >> shift]; };
   const float *kb = reinterpret_cast<const float*>(a.kv.k), *vb = reinterpret_cast<const float*>(a.kv.v);
   // the score of a dot product; exact functions, the sums' errors are of their size
   auto score = [&](float d) { return CAP ? a.cap * tanhf(d * a.scale / a.cap) : d * a.scale; };
+  // one tile's scores of row tile t into weights, and its values added
+  auto add = [&](int t, f32x4 sc, int k0, const bool (&vok)[4], const f32x4 (&vf)[NC]) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      sc[e] = vok[e] && sees(w[t].lim, k0 + 4 * lk + e) ? score(sc[e]) : -INFINITY;
+      mx = vmax(mx, sc[e]);
+    }
+    mx = vmax(mx, __shfl_xor(mx, 16));
+    mx = vmax(mx, __shfl_xor(mx, 32));
+    const float mn = vmax(m[t], mx), ref = mn == -INFINITY ? 0.f : mn, alpha = __expf(m[t] - ref);
+    float ps = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      sc[e] = __expf(sc[e] - ref);
+      ps += sc[e];
+    }
+    l[t] = l[t] * alpha + ps;
+    m[t] = mn;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      o[t][c] *= alpha;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[t][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[c][e], sc[e], o[t][c], 0, 0, 0);
+    }
+  };
   int pk = 0, pv[4] = {0, 0, 0, 0};
   auto request = [&](int u) {
     const int k0 = first_key(u);
@@ -1159,118 +1200,143 @@ __global__ void __launch_bounds__(512) paged_f32_kernel(PagedAttnArgs a) {
     };
     if constexpr (HDP <= 128) load_v();        // (at 256 both would not fit the registers)
     if (u + NW < it.uend) request(u + NW);
-    f32x4 sc = zero;
+    if constexpr (HDP > 128) {
+      // (one row tile: values after the scores)
+      f32x4 sc = zero;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+      for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c][e], qf[c][e], sc, 0, 0, 0);
-    if constexpr (HDP > 128) load_v();
-    float mx = -INFINITY;
+        for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c][e], qf[0][c][e], sc, 0, 0, 0);
+      load_v();
+      add(0, sc, k0, vok, vf);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      sc[e] = vok[e] && sees(w.lim, k0 + 4 * lk + e) ? score(sc[e]) : -INFINITY;
-      mx = vmax(mx, sc[e]);
-    }
-    mx = vmax(mx, __shfl_xor(mx, 16));
-    mx = vmax(mx, __shfl_xor(mx, 32));
-    const float mn = vmax(m, mx), ref = mn == -INFINITY ? 0.f : mn, alpha = __expf(m - ref);
-    float ps = 0.f;
+      for (int t = 0; t < RT; ++t) {
+        f32x4 sc = zero;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      sc[e] = __expf(sc[e] - ref);
-      ps += sc[e];
-    }
-    l = l * alpha + ps;
-    m = mn;
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      o[c] *= alpha;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[c][e], sc[e], o[c], 0, 0, 0);
+          for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c][e], qf[t][c][e], sc, 0, 0, 0);
+        add(t, sc, k0, vok, vf);
+      }
     }
   }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
   // rows with an output that is not finite: again, key by key (as `repair`)
   float z = 0.f;
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
+  for (int t = 0; t < RT; ++t) {
+    l[t] += __shfl_xor(l[t], 16);
+    l[t] += __shfl_xor(l[t], 32);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z = __builtin_fmaf(o[c][e], 0.f, z);
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z = __builtin_fmaf(o[t][c][e], 0.f, z);
+  }
   if (__ballot(z != z) != 0) {
-    const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) o[c] = zero;
+    for (int t = 0; t < RT; ++t) {
+      const float ref = m[t] == -INFINITY ? 0.f : m[t];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) o[t][c] = zero;
 #pragma unroll 1
-    for (int u = it.ubeg + wave; u < it.uend; u += NW) {
-      const int k0 = first_key(u);
+      for (int u = it.ubeg + wave; u < it.uend; u += NW) {
+        const int k0 = first_key(u);
 #pragma unroll 1
-      for (int j = k0; j < min(k0 + KT, it.klim); ++j) {
-        const bool vis = sees(w.lim, j);
-        if (__ballot(vis) == 0) continue;
-        const long off = page_offset(a, it.pages[j >> shift], it.g);
-        if (off < 0) continue;
-        const long at = off + (long)(j & smask) * a.kv.tok_stride;
-        float d = 0.f;
+        for (int j = k0; j < min(k0 + KT, it.klim); ++j) {
+          const bool vis = sees(w[t].lim, j);
+          if (__ballot(vis) == 0) continue;
+          const long off = page_offset(a, it.pages[j >> shift], it.g);
+          if (off < 0) continue;
+          const long at = off + (long)(j & smask) * a.kv.tok_stride;
+          float d = 0.f;
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
-          if (c * 16 + lk * 4 < hd) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(kb + at + c * 16 + lk * 4);
+          for (int c = 0; c < NC; ++c)
+            if (c * 16 + lk * 4 < hd) {
+              const f32x4 x = *reinterpret_cast<const f32x4*>(kb + at + c * 16 + lk * 4);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) d = __builtin_fmaf(x[e], qf[c][e], d);
-          }
-        d += __shfl_xor(d, 16);
-        d += __shfl_xor(d, 32);
-        const float p = __expf(score(d) - ref);
+              for (int e = 0; e < 4; ++e) d = __builtin_fmaf(x[e], qf[t][c][e], d);
+            }
+          d += __shfl_xor(d, 16);
+          d += __shfl_xor(d, 32);
+          const float p = __expf(score(d) - ref);
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
-          if (vis && c * 16 + lk * 4 < hd) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(vb + at + c * 16 + lk * 4);
+          for (int c = 0; c < NC; ++c)
+            if (vis && c * 16 + lk * 4 < hd) {
+              const f32x4 x = *reinterpret_cast<const f32x4*>(vb + at + c * 16 + lk * 4);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[c][e] = __builtin_fmaf(p, x[e], o[c][e]);
-          }
+              for (int e = 0; e < 4; ++e) o[t][c][e] = __builtin_fmaf(p, x[e], o[t][c][e]);
+            }
+        }
       }
     }
   }
-  // merge the waves, the upper half into the lower until wave 0 holds all
-  for (int n = NW / 2; n > 0; n /= 2) {
-    if (wave >= n && wave < 2 * n) {
-      float* dst = mg[wave - n] + lane * REC;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) *reinterpret_cast<f32x4*>(dst + 4 * c) = o[c];
-      dst[HDP / 4] = m;
-      dst[HDP / 4 + 1] = l;
-    }
-    __syncthreads();
-    if (wave < n) {
-      const float* src = mg[wave] + lane * REC;
-      const float m2 = src[HDP / 4], l2 = src[HDP / 4 + 1], mm = vmax(m, m2);
-      // (a wave without keys weighs nothing)
-      const float w1 = m == -INFINITY ? 0.f : __expf(m - mm), w2 = m2 == -INFINITY ? 0.f : __expf(m2 - mm);
+  for (int t = 0; t < RT; ++t) {
+    // merge the waves, the upper half into the lower until wave 0 holds all
+    for (int n = NW / 2; n > 0; n /= 2) {
+      if (wave >= n && wave < 2 * n) {
+        float* dst = mg[wave - n] + lane * REC;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(src + 4 * c);
-        if (w1 != 1.f) o[c] = w1 == 0.f ? zero : o[c] * w1;
-        if (w2 != 0.f) o[c] += x * w2;
+        for (int c = 0; c < NC; ++c) *reinterpret_cast<f32x4*>(dst + 4 * c) = o[t][c];
+        dst[HDP / 4] = m[t];
+        dst[HDP / 4 + 1] = l[t];
       }
-      l = l * w1 + l2 * w2;
-      m = mm;
-    }
-    __syncthreads();
-  }
-  if (wave != 0 || it.row0 + lr >= it.nrows) return;
-  const float inv = inverse(l);
-  const long row = (long)w.tok * a.n_q + w.head;
-  float* op = direct ? reinterpret_cast<float*>(a.o) + (long)w.tok * a.o_ts + (long)w.head * a.o_hs : part_of(a, row, it.slot);
+      __syncthreads();
+      if (wave < n) {
+        const float* src = mg[wave] + lane * REC;
+        const float m2 = src[HDP / 4], l2 = src[HDP / 4 + 1], mm = vmax(m[t], m2);
+        // (a wave without keys weighs nothing)
+        const float w1 = m[t] == -INFINITY ? 0.f : __expf(m[t] - mm), w2 = m2 == -INFINITY ? 0.f : __expf(m2 - mm);
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
-    if (c * 16 + lk * 4 < hd) *reinterpret_cast<f32x4*>(op + c * 16 + lk * 4) = direct ? o[c] * inv : o[c];
-  if (lk != 0) return;
-  if (!direct) {
-    store_stats(a, row, it.slot, m * LOG2E, l);
+        for (int c = 0; c < NC; ++c) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(src + 4 * c);
+          if (w1 != 1.f) o[t][c] = w1 == 0.f ? zero : o[t][c] * w1;
+          if (w2 != 0.f) o[t][c] += x * w2;
+        }
+        l[t] = l[t] * w1 + l2 * w2;
+        m[t] = mm;
+      }
+      __syncthreads();
+    }
+    if (wave == 0 && it.row0 + t * 16 + lr < it.nrows) {
+      const float inv = inverse(l[t]);
+      const long row = (long)w[t].tok * a.n_q + w[t].head;
+      float* op = direct ? reinterpret_cast<float*>(a.o) + (long)w[t].tok * a.o_ts + (long)w[t].head * a.o_hs : part_of(a, row, it.slot);
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (c * 16 + lk * 4 < hd) *reinterpret_cast<f32x4*>(op + c * 16 + lk * 4) = direct ? o[t][c] * inv : o[t][c];
+      if (lk == 0) {
+        if (!direct) {
+          store_stats(a, row, it.slot, m[t] * LOG2E, l[t]);
+        } else {
+          if (a.lse) a.lse[row] = m[t] + logf(l[t]);
+          if (a.slots > 1) store_stats(a, row, 0, 0.f, -1.f);
+        }
+      }
+    }
+  }
+}
+
+template <int HDP, bool CAP, int RT>
+__global__ void __launch_bounds__(512) paged_f32_kernel(PagedAttnArgs a) {
+  __shared__ F32Shared<HDP> sh;
+  f32_body<HDP, CAP, RT, false>(a, sh, blockIdx.x, blockIdx.y);
+}
+
+// As paged_pair_kernel.
+template <int HDP, bool CAP>
+__global__ void __launch_bounds__(512) paged_f32_pair_kernel(PagedAttnArgs a, PagedAttnArgs b) {
+  __shared__ F32Shared<HDP> sh;
+  const int per_a = a.tiles * a.kv.n_kv, na = per_a * a.ranges;
+  int L = blockIdx.x;
+  if (L < na) {
+    const int range = div_by(L, per_a, a.mul_blocks);
+    f32_body<HDP, CAP, 1, true>(a, sh, L - range * per_a, range);
   } else {
-    if (a.lse) a.lse[row] = m + logf(l);
-    if (a.slots > 1) store_stats(a, row, 0, 0.f, -1.f);
+    const int per_b = b.tiles * b.kv.n_kv;
+    L -= na;
+    const int range = div_by(L, per_b, b.mul_blocks);
+    f32_body<HDP, CAP, 1, false>(b, sh, L - range * per_b, range);
   }
 }
 
@@ -1356,12 +1422,14 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a) {
 // ---------------------------------------------------------------- host
 // Rows of a tile, keys of a key tile and key tiles of a round of kernel k at
 // padded head dim hdp.
-static int tile_rows(int k) { return k == PAGED_ROWS8 ? 256 : k == PAGED_ROWS || k == PAGED_ROWS2 ? 128 : 16; }
+static int tile_rows(int k, int hdp) {
+  return k == PAGED_ROWS8 ? 256 : k == PAGED_ROWS || k == PAGED_ROWS2 ? 128 : k == PAGED_F32R ? 16 * f32_row_tiles(hdp) : 16;
+}
 static int tile_keys(int k, int hdp) {
   const int wide = hdp == 256 ? 1 : 2;
-  return k == PAGED_F32 ? 16 : k == PAGED_KEYS ? 16 * wide : 32 * wide;
+  return k == PAGED_F32 || k == PAGED_F32R ? 16 : k == PAGED_KEYS ? 16 * wide : 32 * wide;
 }
-static int round_tiles(int k) { return k == PAGED_KEYS ? 4 : k == PAGED_ROWS2 || k == PAGED_ROWS8 ? 2 : k == PAGED_F32 ? 2 : 1; }
+static int round_tiles(int k) { return k == PAGED_KEYS ? 4 : k == PAGED_ROWS2 || k == PAGED_ROWS8 ? 2 : k == PAGED_F32 || k == PAGED_F32R ? 2 : 1; }
 
 // How long a part would take with kernel p.kernel (us) by a simple model, and
 // the number of key ranges that makes it least: the blocks' start, as many
@@ -1386,11 +1454,12 @@ struct PartShape {
 
 static double cut(PagedPart& p, const PartShape& q) {
   const int w = q.hdp == 64 ? 0 : q.hdp == 128 ? 1 : 2, kt = tile_keys(p.kernel, q.hdp), unit = round_tiles(p.kernel);
-  const int es = p.kernel == PAGED_F32 ? 4 : 2;
+  const bool f32 = p.kernel == PAGED_F32 || p.kernel == PAGED_F32R;
+  const int es = f32 ? 4 : 2;
   // by PagedKernel and padded head dim
-  static const double START[5][3] = {{4, 5, 5}, {5, 7.5, 12}, {4, 4, 4}, {5, 7.5, 12}, {0, 5.5, 0}};
-  static const double ROUND[5][3] = {{1, 1, 1.3}, {1, 1.2, 1.7}, {1, 1, 1}, {1.55, 1.8, 1.9}, {0, 3.1, 0}};
-  static const int RESIDENT[5][3] = {{1024, 512, 512}, {512, 512, 256}, {512, 512, 512}, {256, 256, 256}, {0, 256, 0}};
+  static const double START[6][3] = {{4, 5, 5}, {5, 7.5, 12}, {4, 4, 4}, {5, 7.5, 12}, {0, 5.5, 0}, {4.5, 4.5, 4.5}};
+  static const double ROUND[6][3] = {{1, 1, 1.3}, {1, 1.2, 1.7}, {1, 1, 1}, {1.55, 1.8, 1.9}, {0, 3.1, 0}, {2.5, 2.5, 2.5}};
+  static const int RESIDENT[6][3] = {{1024, 512, 512}, {512, 512, 256}, {512, 512, 512}, {256, 256, 256}, {0, 256, 0}, {256, 256, 256}};
   const long full = std::max(1, (q.keys + kt * unit - 1) / (kt * unit));     // rounds of all keys
   const long total = std::max(1, (q.seen + kt * unit - 1) / (kt * unit));
   const long blocks = (long)p.tiles * q.n_kv, resident = RESIDENT[p.kernel][w];
@@ -1405,13 +1474,13 @@ static double cut(PagedPart& p, const PartShape& q) {
     if ((total + per - 1) / per != s) continue;
     const double on = (double)std::min(blocks * s, resident), per_cu = blocks * s / 256.0, passes = blocks * s / (double)resident;
     const double uneven = per_cu > 1.0 && per_cu <= resident / 256 ? std::ceil(per_cu) / per_cu : 1.0;
-    const double rounds = p.kernel == PAGED_F32 ? (per + 3) / 4 : per;         // (eight waves, a tile each)
+    const double rounds = f32 ? (per + 3) / 4 : per;         // (eight waves, a tile each)
     const double slow = (small && passes > 1.0 ? 1.25 : 1.0) * (small && q.cap ? 1.3 : 1.0);
     const double busy = std::max(rounds * ROUND[p.kernel][w] * slow,
                                  per * bytes * std::max({1e-5, on * differ * uneven / 5e6, on / 15e6}));
     const double t = START[p.kernel][w] + std::ceil(passes) +
                      busy * (q.share < 0.95 ? std::max(1.0, passes * q.share + 0.3) : std::ceil(passes)) +
-                     (small || p.kernel == PAGED_F32 ? 0.5 * rounds : 0.0) +
+                     (small || f32 ? 0.5 * rounds : 0.0) +
                      (n > 1 ? 4.0 + q.rows * (double)n * q.hd * 8 / 2e6 : 0.0);
     if (t < best) { best = t; best_per = s > 1 ? per : full; }
   }
@@ -1427,7 +1496,7 @@ PagedPlan paged_plan(const PagedAttnArgs& a, int et) {
   const long all = (long)a.bt.n_tok * a.G, rows_req = (long)a.bt.max_new * a.G;
   // a part by kernel k: flat: the rows of the batch in one sequence of tiles
   auto part = [&](int k, bool flat, int keys, PagedPart& q) {
-    const int br = tile_rows(k);
+    const int br = tile_rows(k, p.hdp);
     q.kernel = k;
     q.tiles = (int)(flat ? std::max<long>(1, (all + br - 1) / br) : rows_req <= br ? a.bt.n_req : all / br + a.bt.n_req);
     const int seen = a.causal && a.window && !flat ? (int)std::min<long>(keys, (long)a.window + br / a.G + 1) : keys;
@@ -1447,8 +1516,12 @@ PagedPlan paged_plan(const PagedAttnArgs& a, int et) {
   const int rest = a.bt.max_len - a.shared_len;
   p.n_parts = a.shared_len > 0 ? 2 : 1;
   if (et == ET_F32) {
+    // (more rows a block: two prompts of 2000 of 32 heads of 128 1113 -> 883 us, of 3000 of 15 heads of 64 410 -> 349, six
+    // of 700 of 4 heads of 64 30 -> 43; for a common context never faster)
     if (a.shared_len > 0) p.part[0] = least({PAGED_F32}, true, a.shared_len);
-    p.part[p.n_parts - 1] = least({PAGED_F32}, false, rest);
+    PagedPart& last = p.part[p.n_parts - 1];
+    if (a.shared_len == 0 && p.hdp < 256 && rows_req > 16) last = least({PAGED_F32, PAGED_F32R}, false, rest);
+    else last = least({PAGED_F32}, false, rest);
   } else if (a.shared_len > 0) {
     // Up to 32 tiles of 16 rows (128 at head dim 256, where a block of 128 rows takes long to begin and end) the
     // common context goes in those, beyond in tiles of 128: 16 rows x 2 x 8 heads of 128 over 4096 keys 15.7 and 16.9 us,
@@ -1478,19 +1551,18 @@ PagedPlan paged_plan(const PagedAttnArgs& a, int et) {
   return p;
 }
 
-size_t paged_attention_ws(const PagedAttnArgs& a, int et) {
-  const PagedPlan p = paged_plan(a, et);
+size_t paged_attention_ws(const PagedAttnArgs& a, const PagedPlan& p) {
   return p.slots > 1 ? (size_t)a.bt.n_tok * a.n_q * p.slots * (a.kv.hd + 2) * 4 : 0;
 }
 
 template <int HDP, bool CAP>
-static void launch_one(const PagedAttnArgs& a, int kernel, bool flat, hipStream_t s) {
+static void launch_one(const PagedAttnArgs& a, int kernel, hipStream_t s) {
   const dim3 grid((unsigned)a.tiles * a.kv.n_kv, a.ranges);
   if (kernel == PAGED_KEYS) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_KEYS>), grid, dim3(256), 0, s, a);
   else if (HDP == 128 && kernel == PAGED_ROWS8) hipLaunchKernelGGL((paged_kernel<HDP, CAP, HDP == 128 ? PAGED_ROWS8 : PAGED_KEYS>), grid, dim3(512), 0, s, a);
   else if (kernel == PAGED_ROWS2) hipLaunchKernelGGL((paged_kernel<HDP, CAP, PAGED_ROWS2>), grid, dim3(512), 0, s, a);
-  else if (flat) hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP, true>), grid, dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP, false>), grid, dim3(512), 0, s, a);
+  else if (HDP < 256 && kernel == PAGED_F32R) hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP, f32_row_tiles(HDP)>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((paged_f32_kernel<HDP, CAP, 1>), grid, dim3(512), 0, s, a);
 }
 
 // The two parts of a batch with a common context.
@@ -1498,16 +1570,14 @@ template <int HDP, bool CAP>
 static void launch_pair(const PagedAttnArgs& a, const PagedAttnArgs& b, int ka, hipStream_t s) {
   const dim3 grid((unsigned)(a.tiles * a.kv.n_kv * a.ranges + b.tiles * b.kv.n_kv * b.ranges));
   if (ka == PAGED_ROWS) hipLaunchKernelGGL((paged_pair_kernel<HDP, CAP, PAGED_ROWS>), grid, dim3(256), 0, s, a, b);
-  else hipLaunchKernelGGL((paged_pair_kernel<HDP, CAP, PAGED_KEYS>), grid, dim3(256), 0, s, a, b);
+  else if (ka == PAGED_KEYS) hipLaunchKernelGGL((paged_pair_kernel<HDP, CAP, PAGED_KEYS>), grid, dim3(256), 0, s, a, b);
+  else hipLaunchKernelGGL((paged_f32_pair_kernel<HDP, CAP>), grid, dim3(512), 0, s, a, b);
 }
 
 template <int HDP, bool CAP>
 static void launch_parts(const PagedAttnArgs (&a)[2], const PagedPlan& p, hipStream_t s) {
-  if (p.n_parts == 2 && p.part[0].kernel != PAGED_F32) {
-    launch_pair<HDP, CAP>(a[0], a[1], p.part[0].kernel, s);
-    return;
-  }
-  for (int i = 0; i < p.n_parts; ++i) launch_one<HDP, CAP>(a[i], p.part[i].kernel, p.n_parts == 2 && i == 0, s);
+  if (p.n_parts == 2) launch_pair<HDP, CAP>(a[0], a[1], p.part[0].kernel, s);
+  else launch_one<HDP, CAP>(a[0], p.part[0].kernel, s);
 }
 
 template <typename T, int LPR>
@@ -1524,9 +1594,8 @@ static void launch_merge(const PagedAttnArgs& a, int hdp, long rows, hipStream_t
   else launch_merge<T, 64>(a, rows, s);
 }
 
-void launch_paged_attention(const PagedAttnArgs& a, int et, hipStream_t s) {
+void launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& p, int et, hipStream_t s) {
   if (a.bt.n_tok <= 0 || a.bt.max_new <= 0) return;
-  const PagedPlan p = paged_plan(a, et);
   auto mul = [](long d) { return d == 1 ? 0u : (unsigned)(((1ull << 32) + d - 1) / d); };
   PagedAttnArgs part[2] = {a, a};
   int slot = 0;

@@ -55,14 +55,14 @@ struct PagedAttnArgs {
 // head of the group), its waves split the keys; PAGED_ROWS: its waves split 128
 // rows; PAGED_ROWS2: so do two groups of waves, which split the keys;
 // PAGED_ROWS8: eight waves split 256 rows; PAGED_F32: fp32, 16 rows, waves
-// split the keys. One part over the cache, or two: the common context (all rows
+// split the keys, PAGED_F32R: 64 rows (32 at head dim 128). One part over the cache, or two: the common context (all rows
 // of the batch in one sequence of tiles) and what follows it.
-enum PagedKernel { PAGED_KEYS = 0, PAGED_ROWS = 1, PAGED_F32 = 2, PAGED_ROWS2 = 3, PAGED_ROWS8 = 4 };
+enum PagedKernel { PAGED_KEYS = 0, PAGED_ROWS = 1, PAGED_F32 = 2, PAGED_ROWS2 = 3, PAGED_ROWS8 = 4, PAGED_F32R = 5 };
 struct PagedPart { int kernel, tiles, chunk, ranges; };
 struct PagedPlan { int n_parts, hdp, slots; PagedPart part[2]; };
 PagedPlan paged_plan(const PagedAttnArgs& a, int et);
-size_t paged_attention_ws(const PagedAttnArgs& a, int et);
-void launch_paged_attention(const PagedAttnArgs& a, int et, hipStream_t s);
+size_t paged_attention_ws(const PagedAttnArgs& a, const PagedPlan& p);
+void launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& p, int et, hipStream_t s);
 
 // ---------------------------------------------------------------- device side
 struct ReqSpan { int first, n, len; };         // first row, new tokens, tokens in the cache

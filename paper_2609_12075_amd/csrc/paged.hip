@@ -115,11 +115,12 @@ vla_status attend(const vla_kv_pool* p, const vla_ragged* b, const vla_attention
                   hipStream_t s) {
   return guarded([&] {
     const PagedAttnArgs a = attention_args(p, b, t, shared, shared_len, true);
-    const size_t need = paged_attention_ws(a, p->dtype);
+    const PagedPlan plan = paged_plan(a, p->dtype);
+    const size_t need = paged_attention_ws(a, plan);
     VLA_REQUIRE(need == 0 || (t->ws && t->ws_bytes >= need && aligned(t->ws, 16)),
                 "this attention needs " + std::to_string(need) + " bytes of 16-byte aligned scratch");
     DeviceGuard g(p->device);
-    launch_paged_attention(a, p->dtype, s);
+    launch_paged_attention(a, plan, p->dtype, s);
     VLA_HIP(hipGetLastError());
   });
 }
@@ -173,7 +174,8 @@ vla_status vla_attention_workspace(const vla_kv_pool* p, const vla_ragged* b, co
                                    int shared_len, size_t* bytes) {
   return guarded([&] {
     VLA_REQUIRE(bytes != nullptr, "null bytes");
-    *bytes = paged_attention_ws(attention_args(p, b, t, shared_len != 0, shared_len, false), p->dtype);
+    const PagedAttnArgs a = attention_args(p, b, t, shared_len != 0, shared_len, false);
+    *bytes = paged_attention_ws(a, paged_plan(a, p->dtype));
   });
 }
 

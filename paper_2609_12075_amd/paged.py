@@ -264,4 +264,4 @@ def attention_plan(n_req: int, n_tok: int, max_new: int, max_len: int, n_q: int,
     plan = (_ci * 9)()
     vla._check(_lib().vla_debug_paged_plan(ctypes.byref(pool), ctypes.byref(batch), ctypes.byref(a), shared_len, plan))
     parts = [tuple(plan[1 + 4 * i:5 + 4 * i]) for i in range(2) if plan[1 + 4 * i] >= 0]
-    return {"hdp": plan[0], "parts": [(("keys", "rows", "f32", "rows2", "rows8")[p[0]],) + p[1:] for p in parts]}
+    return {"hdp": plan[0], "parts": [(("keys", "rows", "f32", "rows2", "rows8", "f32_rows")[p[0]],) + p[1:] for p in parts]}

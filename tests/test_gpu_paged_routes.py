@@ -22,6 +22,10 @@ ROUTES = [
     (([300, 30], [2500, 2100], (8, 2, 128), 8), "rows2", "split"),
     (([300, 30], [2500, 1900], (8, 2, 256), 16), "rows2", "split"),
     (([900, 77, 523], [1200, 300, 600], (16, 8, 64), 1), "rows2", 1),
+    # fp32: 16 rows a block, 64 or 32
+    (([20, 3, 17], [600, 333, 17], (8, 2, 72), 2), "f32", "split"),
+    (([300, 222], [320, 400], (32, 8, 128), 4), "f32_rows", 1),
+    (([400, 222], [1620, 1400], (15, 5, 64), 16), "f32_rows", "split"),
     # 256 rows
     (([300, 290, 280, 299, 271, 300], [300, 310, 280, 299, 271, 333], (32, 32, 128), 1), "rows8", 1),
     (([250, 249, 250, 240, 233, 250], [250, 349, 250, 310, 233, 350], (32, 32, 72), 64), "rows8", 1),
@@ -34,9 +38,10 @@ MASKS = [dict(), dict(cap=20.0), dict(causal=False), dict(window=70, prefix="som
 @pytest.mark.parametrize("shape,kernel,ranges", ROUTES, ids=lambda x: str(x))
 def test_routes(shape, kernel, ranges, mask):
     new, length, (n_q, n_kv, hd), page = shape
-    c = U.Case(new, length, n_q, n_kv, hd, page=page, seed=31, extra_rows=2)
+    f32 = kernel.startswith("f32")
+    c = U.Case(new, length, n_q, n_kv, hd, dtype="f32" if f32 else "bf16", page=page, seed=31, extra_rows=2)
     if not mask:                                       # (a mask can change the choice)
-        p = paged.attention_plan(len(new), c.rows, max(new), max(length), n_q, n_kv, hd, page)
+        p = paged.attention_plan(len(new), c.rows, max(new), max(length), n_q, n_kv, hd, page, bf16=not f32)
         k = p["parts"][0]
         assert len(p["parts"]) == 1 and (k[0], "split" if k[3] > 1 else 1) == (kernel, ranges), p
         c.table[0][len(c.table[0]) // 3] = -1          # a page that is not there
