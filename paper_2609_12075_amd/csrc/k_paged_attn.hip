@@ -624,6 +624,11 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kg = wave / NWR, wr = wave % NWR;
   const int lq = lane & 31, h = lane >> 5, hd = a.kv.hd, shift = a.kv.page_shift;
+  // (the window's first page numbers go out ahead of the queries: loads return in order)
+  auto first_key = [&](int u) { return a.klo + (u < it.n1 ? u : u - it.n1 + it.t2) * KT; };
+  const int nrounds = (it.uend - it.ubeg + RTL - 1) / RTL;
+  int w0 = nrounds > 0 ? first_key(it.ubeg) >> shift : 0, guessed = 0;
+  if (nrounds > 0 && tid < PW) guessed = it.pages[min(w0 + tid, (it.klim - 1) >> shift)];
   const int wrow = it.row0 + wr * 32;
   const bool active = wrow < it.nrows;
   const Row w = row_of<FLAT>(a, it, wrow + lq);
@@ -642,10 +647,8 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
   s.l = 0.f;
   const float sl2 = a.scale * LOG2E, c1 = CAP ? 2.f * sl2 / a.cap : 0.f, c2 = a.cap * LOG2E;
 
-  auto first_key = [&](int u) { return a.klo + (u < it.n1 ? u : u - it.n1 + it.t2) * KT; };
   const char *kb = reinterpret_cast<const char*>(a.kv.k), *vb = reinterpret_cast<const char*>(a.kv.v);
   const unsigned ring = lds_addr(smem);
-  int w0 = 0;
   bool holes = false;
   Mover<HDP, SUB * KT, NWR> mv(a, win, wr);
   auto issue = [&](int p) {                    // round p
@@ -655,10 +658,8 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
     mv.rows(first_key(u), w0, it.klim);
     mv.template load<true>(kb, vb, dst, dst + TILE);
   };
-  const int nrounds = (it.uend - it.ubeg + RTL - 1) / RTL;
   if (nrounds > 0) {
-    w0 = first_key(it.ubeg) >> shift;
-    holes = fill_window<64 * NWR * KS>(a, it, win, w0);
+    holes = fill_window<64 * NWR * KS>(a, it, win, w0, w0, guessed);
     issue(0);
   }
   hold<NC, 16>(8 * h, hd, hd == HDP, qf);

@@ -11,6 +11,7 @@ current stream.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import Optional, Sequence
 
 import torch
@@ -129,7 +130,7 @@ def _rows(t, name, pool: KVPool, batch: Batch, heads: int):
     """Checks a token buffer [n_tok][heads][head_dim] and returns (address, token stride, head stride)."""
     if t.shape != (batch.n_tok, heads, pool.head_dim):
         raise ValueError(f"{name} must be [{batch.n_tok}, {heads}, {pool.head_dim}], not {tuple(t.shape)}")
-    if t.dtype != pool.dtype or t.device != pool.device:
+    if t.dtype is not pool.dtype or t.get_device() != pool.index:
         raise ValueError(f"{name} must be {pool.dtype} on {pool.device}, not {t.dtype} on {t.device}")
     ts, hs, ds = t.stride()
     if ds != 1 and pool.head_dim > 1:
@@ -166,6 +167,11 @@ def _empty(shape, dtype, pool: KVPool, stream):
         return torch.empty(shape, dtype=dtype, device=pool.device)
 
 
+@functools.lru_cache(maxsize=64)
+def _sections(s):
+    return (_ci * 3)(*s)
+
+
 def append(pool: KVPool, batch: Batch, k, v, q=None, q_out=None, positions=None, sections: Sequence[int] = (),
            rope_base: float = 10000.0, stream=None):
     """vla_kv_append. k, v [n_tok][n_kv][head_dim], q [n_tok][n_q][head_dim]
@@ -186,8 +192,8 @@ def append(pool: KVPool, batch: Batch, k, v, q=None, q_out=None, positions=None,
     kp, kt, kh = _rows(k, "k", pool, batch, pool.n_kv)
     vp, vt, vh = _rows(v, "v", pool, batch, pool.n_kv)
     pos = None if positions is None else _i32(positions, "positions", (batch.n_tok, n), pool.device)
-    a = AppendArgsC(kp, vp, kt, kh, vt, vh, n_q, qr[0], qo[0], qr[1], qr[2], qo[1], qo[2], n, tuple(sections), pos,
-                    rope_base)
+    a = AppendArgsC(kp, vp, kt, kh, vt, vh, n_q, qr[0], qo[0], qr[1], qr[2], qo[1], qo[2], n, _sections(tuple(sections)),
+                    pos, rope_base)
     vla._check(_lib().vla_kv_append(pool.ref, batch.ref, ctypes.byref(a), _stream(pool, stream)))
     return q_out
 
