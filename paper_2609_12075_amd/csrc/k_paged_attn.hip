@@ -260,12 +260,12 @@ __device__ __forceinline__ unsigned lds_addr(const void* p) {
 // compiler, which cannot tell the slots of a ring apart, waits for all of its
 // own direct loads before each LDS read; these loads' waits are in the loops.
 __device__ __forceinline__ void dma16(const void* src, unsigned dst) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(dst) : "memory");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(dst) : "memory", "m0");
 }
 
 // The same from a wave-uniform base and 32-bit offsets of the lanes.
 __device__ __forceinline__ void dma16(const char* base, unsigned off, unsigned dst) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(dst) : "memory");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(dst) : "memory", "m0");
 }
 
 // V^T fragments of a 16-key group: subtile u (32 dims) holds, of lane l, dim

@@ -74,7 +74,8 @@ void fill(const vla_kv_pool* p, const vla_ragged* b, bool buffers, PagedKV& kv, 
   kv.page_stride = p->page_stride; kv.head_stride = p->head_stride; kv.tok_stride = p->token_stride;
   kv.n_kv = p->n_kv; kv.hd = p->head_dim; kv.n_pages = p->n_pages; kv.page_shift = __builtin_ctz(p->page_tokens);
   bt.start = b->start; bt.kv_len = b->kv_len; bt.pages = b->pages;
-  bt.n_req = b->n_req; bt.n_tok = b->n_tok; bt.max_new = b->max_new; bt.max_len = b->max_len;
+  // (no request brings more than all tokens; products with it stay below 2^30)
+  bt.n_req = b->n_req; bt.n_tok = b->n_tok; bt.max_new = std::min(b->max_new, b->n_tok); bt.max_len = b->max_len;
   bt.pages_stride = b->pages_stride;
 }
 

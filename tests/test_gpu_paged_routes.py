@@ -130,3 +130,29 @@ def test_two_streams_and_threads_of_calls():
         for x in got[i]:
             assert torch.equal(x, want[i])
 
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_loose_bounds_and_empty_batches(dtype):
+    """max_new far over what any request can bring; a batch without tokens; caches without a page."""
+    c = U.Case([3, 1, 40], [30, 200, 77], 8, 2, 64, dtype=dtype, page=16, seed=50)
+    pool, _, q = c.device()
+    ref = U.attention_ref(c)
+    U.check_attention(c, paged.attention(pool, c.batch(max_new=2 ** 31 - 1), q), ref)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")   # noqa: E731
+    none = paged.Batch(i32([0, 0]), i32([20]), i32([c.table[0]]), 0, 0, 20)
+    empty = q[:0]
+    assert paged.attention(pool, none, empty).shape == empty.shape
+    assert paged.shared_attention(pool, none, empty, 16).shape == empty.shape
+    k = torch.zeros(0, 2, 64, dtype=q.dtype, device="cuda")
+    before = pool.k.clone()
+    assert paged.append(pool, none, k, k, q=empty, sections=[32]).shape == empty.shape
+    no_pages = paged.Batch(i32([0, 2]), i32([0]), torch.zeros(1, 0, dtype=torch.int32, device="cuda"), 2, 2, 0)
+    lse = torch.zeros(2, 8, device="cuda")
+    out = paged.attention(pool, no_pages, q[:2], lse=lse)
+    assert (out == 0).all() and (lse == -float("inf")).all()
+    out = paged.attention(pool, no_pages, q[:2], causal=False)
+    assert (out == 0).all()
+    paged.append(pool, no_pages, k.new_ones(2, 2, 64), k.new_ones(2, 2, 64))
+    torch.cuda.synchronize()
+    assert torch.equal(before, pool.k)

@@ -214,6 +214,8 @@ def test_plans_without_a_gpu_and_the_bounds_of_one_call():
     p = paged.attention_plan(1, 1, 1, 881, 8, 1, 256, page=64)
     assert p["hdp"] == 256 and p["parts"][0][0] == "keys" and p["parts"][0][3] > 1
     assert [k[0] for k in paged.attention_plan(8, 8, 1, 900, 4, 4, 64, shared_len=512, bf16=False)["parts"]] == ["f32"] * 2
+    # no request brings more than the batch's tokens
+    assert paged.attention_plan(4, 16, 2 ** 31 - 1, 900, 8, 2, 64) == paged.attention_plan(4, 16, 16, 900, 8, 2, 64)
     for kw in (dict(bf16=True), dict(bf16=False)):
         with pytest.raises(vla.VlaError, match="too many rows"):
             paged.attention_plan(65535, 65535, 1, 64, 4096, 4096, 64, **kw)
