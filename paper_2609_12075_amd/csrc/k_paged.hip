@@ -1,5 +1,5 @@
-// Paged key/value cache on gfx950: appending to it with the rotation applied
-// on the way, and attention over it.
+// Paged key/value cache on gfx950: appending to it, with the rotation applied
+// on the way.
 #include <algorithm>
 
 #include "paged.h"
@@ -39,7 +39,9 @@ __device__ __forceinline__ void store8(void* p, long i, const float (&x)[8]) {
 // One block per token. Pair f turns by pos * base^(-f / half): the angle in
 // turns is formed and reduced in fp64, so that far positions keep their
 // fraction (pos 2^31 leaves 2^-22 of a turn), and its sine and cosine are
-// fp32. They are the same for all heads: computed once into LDS.
+// fp32. They are the same for all heads: computed once into LDS. Bound by the
+// rows read and written once (7261 tokens of 48 heads of 128: 178.5 MB in 36.6
+// us, 4.9 TB/s, what a large copy moves), single tokens by the launch (3 us).
 template <typename T>
 __global__ void __launch_bounds__(256) append_kernel(AppendArgs a) {
   __shared__ float cs[128], sn[128];

@@ -2,8 +2,8 @@
 //
 // Rows are (token, query head of a KV head's group) pairs in token-major
 // order, so the query heads that share a KV head read its keys once and a tile
-// of rows spans few places. Both products run on the matrix cores (bf16:
-// v_mfma_f32_32x32x16, 32 rows a wave). The scores are computed transposed
+// of rows spans few places. Both products run on the matrix cores (bf16: 16 x 16
+// tiles where rows are few, 32 x 32 in prompts). The scores are computed transposed
 // (S^T = K Q^T): a lane holds keys of one row only, so the row statistics need
 // one exchange between the lane halves, and the probabilities are the second
 // product's operand as they are (its key order inside 16 keys permuted alike
@@ -596,6 +596,12 @@ __device__ __forceinline__ void put_stats(const PagedAttnArgs& a, const Item& it
 // (64 keys a tile; 32 at head dim 256.) Eight waves of rows and two tiles a
 // round where there are rows enough: half the loads and round overhead of four.
 // Two groups of four where the blocks are few: their results meet in LDS.
+// A prompt of 8191 of 32 heads of 128, causal: 529-545 us, 1.03 PFLOP/s at the
+// 1.9 GHz to which the chip throttles (a product of 8192^3 reaches 1.42): the
+// matrix pipe is busy for 42 % of the time, the vector pipe for 40 % (a wave's
+// softmax of a tile takes as long as its products). Measured slower: the scores of
+// the next tile between the weights of this one (700 us), the two waves of a
+// SIMD a barrier apart, one in its products and one in its softmax (711).
 template <int HDP, int KS, int NWR>
 struct RowsShared {
   static constexpr int KT = HDP == 256 ? 32 : 64, SUB = NWR / 4, RING = 2 * KS * SUB * 2 * KT * Lay<HDP>::ROWB;
@@ -680,60 +686,60 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
     }
 #pragma unroll 1
     for (int sub = 0; sub < SUB; ++sub) {
-    const int u = it.ubeg + p * RTL + kg * SUB + sub, k0 = first_key(u);
-    if (!active || u >= it.uend || tile_unseen(wl, k0, k0 + KT)) continue;
-    unsigned kt = ring + (p & 1) * ROUND + kg * 2 * TILE + sub * (KT * Y::ROWB) + ka, vt = kt - ka + TILE + va;
-    asm volatile("" : "+v"(kt), "+v"(vt));
-    // fragments are requested well ahead of their products (LDS answers after
-    // a few of these): all keys' first, two groups of the values' before the
-    // softmax (head dim 256 has no registers for that)
-    f32x16 sc[NS];
-    bf16x8 kf[HDP <= 128 ? NS : 1][NC];
-    constexpr bool AHEAD = HDP <= 128;
-    if constexpr (AHEAD) {
+      const int u = it.ubeg + p * RTL + kg * SUB + sub, k0 = first_key(u);
+      if (!active || u >= it.uend || tile_unseen(wl, k0, k0 + KT)) continue;
+      unsigned kt = ring + (p & 1) * ROUND + kg * 2 * TILE + sub * (KT * Y::ROWB) + ka, vt = kt - ka + TILE + va;
+      asm volatile("" : "+v"(kt), "+v"(vt));
+      // fragments are requested well ahead of their products (LDS answers after
+      // a few of these): all keys' first, two groups of the values' before the
+      // softmax (head dim 256 has no registers for that)
+      f32x16 sc[NS];
+      bf16x8 kf[HDP <= 128 ? NS : 1][NC];
+      constexpr bool AHEAD = HDP <= 128;
+      if constexpr (AHEAD) {
 #pragma unroll
-      for (int st = 0; st < NS; ++st)
+        for (int st = 0; st < NS; ++st)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) kf[st][c] = read_k(kt, c, st * 32 * Y::ROWB);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    // (at head dim 256 the products go first: five capped prompts of 866 tokens 48.4 -> 47.0 us; at 64 and 128,
-    // where the softmax is the longer part, the other way round)
-    if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-    for (int st = 0; st < NS; ++st) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sc[st][i] = 0.f;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        if constexpr (!AHEAD) kf[0][c] = read_k(kt, c, st * 32 * Y::ROWB);
-        sc[st] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[AHEAD ? st : 0][c], qf[c], sc[st], 0, 0, 0);
+          for (int c = 0; c < NC; ++c) kf[st][c] = read_k(kt, c, st * 32 * Y::ROWB);
+        __builtin_amdgcn_sched_barrier(0);
       }
-    }
-    if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(0);
-    bf16x8 vf[2][ND];
-    auto values = [&](int c) {
+      // (at head dim 256 the products go first: five capped prompts of 866 tokens 48.4 -> 47.0 us; at 64 and 128,
+      // where the softmax is the longer part, the other way round)
+      if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int u2 = 0; u2 < ND; ++u2) vf[c % 2][u2] = read_vt<HDP>(vt, u2, c * 16 * Y::ROWB);
-    };
-    if constexpr (AHEAD) {
-      values(0);
-      values(1);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    softmax_tile<HDP, NS, CAP>(s, sc, sl2, c1, c2, !holes && tile_full(wl, k0, k0 + KT), w.lim, k0, a, it, holes);
-    if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(1);
+      for (int st = 0; st < NS; ++st) {
 #pragma unroll
-    for (int c = 0; c < KT / 16; ++c) {
-      const bf16x8 pf = weights_of(sc[c / 2], c % 2);
-      if constexpr (!AHEAD) values(c);
+        for (int i = 0; i < 16; ++i) sc[st][i] = 0.f;
 #pragma unroll
-      for (int u2 = 0; u2 < ND; ++u2)
-        s.o[u2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c % 2][u2], pf, s.o[u2], 0, 0, 0);
-      if constexpr (AHEAD)
-        if (c + 2 < KT / 16) values(c + 2);
-    }
-    if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(0);
+        for (int c = 0; c < NC; ++c) {
+          if constexpr (!AHEAD) kf[0][c] = read_k(kt, c, st * 32 * Y::ROWB);
+          sc[st] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[AHEAD ? st : 0][c], qf[c], sc[st], 0, 0, 0);
+        }
+      }
+      if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(0);
+      bf16x8 vf[2][ND];
+      auto values = [&](int c) {
+#pragma unroll
+        for (int u2 = 0; u2 < ND; ++u2) vf[c % 2][u2] = read_vt<HDP>(vt, u2, c * 16 * Y::ROWB);
+      };
+      if constexpr (AHEAD) {
+        values(0);
+        values(1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      softmax_tile<HDP, NS, CAP>(s, sc, sl2, c1, c2, !holes && tile_full(wl, k0, k0 + KT), w.lim, k0, a, it, holes);
+      if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int c = 0; c < KT / 16; ++c) {
+        const bf16x8 pf = weights_of(sc[c / 2], c % 2);
+        if constexpr (!AHEAD) values(c);
+#pragma unroll
+        for (int u2 = 0; u2 < ND; ++u2)
+          s.o[u2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c % 2][u2], pf, s.o[u2], 0, 0, 0);
+        if constexpr (AHEAD)
+          if (c + 2 < KT / 16) values(c + 2);
+      }
+      if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(0);
     }
   }
   s.l = sum_x32(s.l);
@@ -798,10 +804,13 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
 // V slot of its own and waits for its own loads only: no barrier in the loop,
 // and a slot is loaded again as soon as its fragments are in registers. The
 // waves' (max, sum, output) meet in LDS at the end. For single tokens, whose
-// time is that of the keys' and values' bytes, or where those are few, of the
-// chain of memory round trips and of the instructions (cold in each launch):
-// hence 16-row products (v_mfma_f32_16x16x32), which for the usual few query
-// heads a KV head leave half the registers and code of the 32-row ones.
+// time is that of the keys' and values' bytes (64 tokens over 5060 keys of 8
+// heads of 128 on average: 1.42 GB in 259 us, 5.5 TB/s, where a copy of 4 GB
+// moves 4.8), or where those are few, of the chain of memory round trips and of
+// the instructions (cold in each launch; one token over 881 keys of 8 heads of
+// 256: 8 us and 3.5 for the merge): hence 16-row products
+// (v_mfma_f32_16x16x32), which for the usual few query heads a KV head leave
+// half the registers and code of the 32-row ones.
 // Lane l holds of S^T the keys 16 st + 4 (l / 16) + 0..3 of row l % 16, which
 // is key slot order 4 (l / 16) + 0..3, 16 + 4 (l / 16) + 0..3 of the second product.
 __device__ __forceinline__ float max_x16(float v) {
