@@ -598,7 +598,7 @@ __device__ __forceinline__ void put_stats(const PagedAttnArgs& a, const Item& it
 // Two groups of four where the blocks are few: their results meet in LDS.
 // A prompt of 8191 of 32 heads of 128, causal: 529-545 us, 1.03 PFLOP/s at the
 // 1.9 GHz to which the chip throttles (a product of 8192^3 reaches 1.42): the
-// matrix pipe is busy for 42 % of the time, the vector pipe for 40 % (a wave's
+// matrix pipe is busy for 46 % of the time, the vector pipe for 44 % (a wave's
 // softmax of a tile takes as long as its products). Measured slower: the scores of
 // the next tile between the weights of this one (700 us), the two waves of a
 // SIMD a barrier apart, one in its products and one in its softmax (711).
