@@ -30,18 +30,18 @@ vla_status guarded(F&& f) {
 
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
-// A stride of rows that 16-byte accesses reach; not looked at where `extent` is 1.
-void check_stride(int64_t st, int extent, int hd, int es, const char* what) {
+// A stride of rows that 16-byte accesses reach; not looked at where `extent` is 1. (`what` and `along` make the message)
+void check_stride(int64_t st, int extent, int hd, int es, const char* what, const char* along) {
   if (extent <= 1) return;
   VLA_REQUIRE(st >= hd && st * es % 16 == 0,
-              std::string(what) + " stride must be at least head_dim and a multiple of 16 bytes");
+              std::string(what) + along + " stride must be at least head_dim and a multiple of 16 bytes");
 }
 
 void check_rows(const void* p, int64_t ts, int64_t hs, int rows, int heads, int hd, int es, const char* what) {
   VLA_REQUIRE(p != nullptr || rows == 0, std::string("null ") + what);
   VLA_REQUIRE(aligned(p, 16), std::string(what) + " must be 16-byte aligned");
-  check_stride(ts, rows, hd, es, (std::string(what) + " token").c_str());
-  check_stride(hs, heads, hd, es, (std::string(what) + " head").c_str());
+  check_stride(ts, rows, hd, es, what, " token");
+  check_stride(hs, heads, hd, es, what, " head");
 }
 
 void fill(const vla_kv_pool* p, const vla_ragged* b, bool buffers, PagedKV& kv, RaggedBatch& bt) {
@@ -58,16 +58,16 @@ void fill(const vla_kv_pool* p, const vla_ragged* b, bool buffers, PagedKV& kv, 
   VLA_REQUIRE(b->pages_stride >= 0 && (int64_t)b->pages_stride * p->page_tokens >= b->max_len,
               "max_len tokens do not fit into pages_stride pages");
   const int es = (int)elem_size(p->dtype);
-  check_stride(p->page_stride, p->n_pages, p->head_dim, es, "pool page");
-  check_stride(p->head_stride, p->n_kv, p->head_dim, es, "pool head");
-  check_stride(p->token_stride, p->page_tokens, p->head_dim, es, "pool token");
+  check_stride(p->page_stride, p->n_pages, p->head_dim, es, "pool", " page");
+  check_stride(p->head_stride, p->n_kv, p->head_dim, es, "pool", " head");
+  check_stride(p->token_stride, p->page_tokens, p->head_dim, es, "pool", " token");
   VLA_REQUIRE(p->page_tokens == 1 || p->token_stride * es < (1LL << 28), "pool token stride must be below 2^28 bytes");
   if (buffers) {
     VLA_REQUIRE(p->k && p->v && aligned(p->k, 16) && aligned(p->v, 16), "pool k and v must be 16-byte aligned buffers");
     VLA_REQUIRE(b->start && b->kv_len && (b->pages || b->pages_stride == 0), "null start, kv_len or pages");
     VLA_REQUIRE(aligned(b->start, 4) && aligned(b->kv_len, 4) && aligned(b->pages, 4), "start, kv_len and pages must be 4-byte aligned");
-    int ndev = 0;
-    VLA_HIP(hipGetDeviceCount(&ndev));
+    static int ndev = 0;                       // (does not change while the process runs)
+    if (ndev == 0) VLA_HIP(hipGetDeviceCount(&ndev));
     VLA_REQUIRE(p->device >= 0 && p->device < ndev, "device " + std::to_string(p->device) + " not present");
   }
   kv.k = p->k; kv.v = p->v;

@@ -76,7 +76,7 @@ def _dtype(t) -> int:
 
 
 def _i32(t, name, shape, device):
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name} must be a contiguous int32 tensor {shape} on {device}, "
                          f"not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
@@ -116,7 +116,7 @@ class Batch:
         if pages.dim() != 2:
             raise ValueError("pages must be 2-d")
         self.start, self.kv_len, self.pages = start, kv_len, pages
-        self.device, self.n_req, self.n_tok = dev, n, n_tok
+        self.device, self.index, self.n_req, self.n_tok = dev, dev.index, n, n_tok
         self.c = RaggedC(n, n_tok, max_new, max_len, _i32(start, "start", (n + 1,), dev),
                          _i32(kv_len, "kv_len", (n,), dev), _i32(pages, "pages", (n, pages.shape[1]), dev),
                          pages.shape[1])
@@ -145,7 +145,7 @@ def _heads(q):
 
 
 def _same_device(pool: KVPool, batch: Batch):
-    if batch.device != pool.device:
+    if batch.index != pool.index:
         raise ValueError(f"the batch is on {batch.device}, the pool on {pool.device}")
 
 
@@ -194,7 +194,7 @@ def append(pool: KVPool, batch: Batch, k, v, q=None, q_out=None, positions=None,
     pos = None if positions is None else _i32(positions, "positions", (batch.n_tok, n), pool.device)
     a = AppendArgsC(kp, vp, kt, kh, vt, vh, n_q, qr[0], qo[0], qr[1], qr[2], qo[1], qo[2], n, _sections(tuple(sections)),
                     pos, rope_base)
-    vla._check(_lib().vla_kv_append(pool.ref, batch.ref, ctypes.byref(a), _stream(pool, stream)))
+    vla._check((_L or _lib()).vla_kv_append(pool.ref, batch.ref, ctypes.byref(a), _stream(pool, stream)))
     return q_out
 
 
