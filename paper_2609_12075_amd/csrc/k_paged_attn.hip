@@ -1487,7 +1487,7 @@ static double cut(PagedPart& p, const PartShape& q) {
     const double rounds = f32 ? (per + 3) / 4 : per;         // (eight waves, a tile each)
     const double slow = (small && passes > 1.0 ? 1.25 : 1.0) * (small && q.cap ? 1.3 : 1.0);
     const double busy = std::max(rounds * ROUND[p.kernel][w] * slow,
-                                 per * bytes * std::max({1e-5, on * differ * uneven / 5e6, on / 15e6}));
+                                 per * bytes * std::max({1e-5, on * differ * uneven / 5e6, on / (f32 ? 15e6 : 20e6)}));
     const double t = START[p.kernel][w] + std::ceil(passes) +
                      busy * (q.share < 0.95 ? std::max(1.0, passes * q.share + 0.3) : std::ceil(passes)) +
                      (small || f32 ? 0.5 * rounds : 0.0) +

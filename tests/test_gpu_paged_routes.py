@@ -18,7 +18,7 @@ ROUTES = [
     (([500, 1, 99], [900, 700, 99], (8, 2, 64), 16), "keys", 1),
     (([12, 1, 30], [200, 180, 30], (12, 12, 72), 1), "keys", 1),
     # 128 rows and two key groups: one range and more
-    (([300, 30], [1500, 700], (8, 2, 64), 4), "rows2", "split"),
+    (([470, 30], [1500, 700], (8, 2, 64), 4), "rows2", "split"),
     (([300, 30], [2500, 2100], (8, 2, 128), 8), "rows2", "split"),
     (([300, 30], [2500, 1900], (8, 2, 256), 16), "rows2", "split"),
     (([900, 77, 523], [1200, 300, 600], (16, 8, 64), 1), "rows2", 1),
