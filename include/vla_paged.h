@@ -65,7 +65,8 @@ typedef struct {
  * within the buffers where they do not (the results of such requests are
  * unspecified). An entry of `pages` outside [0, n_pages) is a page that is not
  * there: nothing is appended to it and no one sees its keys (pages that a
- * window has left behind may be given back and marked -1).
+ * window has left behind may be given back and marked -1). Requests may share
+ * pages; two tokens that one call appends may not share a slot.
  */
 typedef struct {
   int n_req;                 /* >= 1 */
@@ -119,7 +120,7 @@ typedef struct {
   float* lse;                /* device [n_tok][n_q], written with ln of the softmax's sum (-inf: no key); or NULL */
   int n_q;                   /* a multiple of n_kv */
   float scale;               /* > 0, or 0 for 1 / sqrt(head_dim) */
-  float cap;                 /* >= 0; 0: no cap */
+  float cap;                 /* 0: no cap; else >= 1e-6, with bf16 <= 1e4 (a score is off by a few 2^-24 of it) */
   int causal;                /* 0 or 1 */
   int window;                /* >= 0; 0: none; needs causal */
   const int32_t* prefix;     /* device [n_req], or NULL (none); needs causal */

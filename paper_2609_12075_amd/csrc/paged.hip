@@ -88,7 +88,10 @@ PagedAttnArgs attention_args(const vla_kv_pool* p, const vla_ragged* b, const vl
   VLA_REQUIRE(t->n_q >= 1 && t->n_q <= 4096 && t->n_q % p->n_kv == 0, "n_q must be a multiple of n_kv in [1, 4096]");
   VLA_REQUIRE((long)b->n_tok * t->n_q < (1L << 30), "n_tok * n_q must be below 2^30");
   VLA_REQUIRE(t->scale >= 0.f && std::isfinite(t->scale), "scale must be positive, or 0 for 1 / sqrt(head_dim)");
+  // (bf16: a capped score is off by a few 2^-24 of the cap, see `capped`)
   VLA_REQUIRE(t->cap >= 0.f && std::isfinite(t->cap), "cap must be >= 0");
+  VLA_REQUIRE(t->cap == 0.f || (t->cap >= 1e-6f && (t->cap <= 1e4f || p->dtype == VLA_F32)),
+              "cap must be 0, or at least 1e-6 and (bf16) at most 1e4");
   VLA_REQUIRE(t->causal == 0 || t->causal == 1, "causal must be 0 or 1");
   VLA_REQUIRE(t->window >= 0 && (t->window == 0 || t->causal), "window must be >= 0 and needs causal");
   VLA_REQUIRE(!t->prefix || t->causal, "prefix needs causal");

@@ -156,3 +156,10 @@ def test_loose_bounds_and_empty_batches(dtype):
     paged.append(pool, no_pages, k.new_ones(2, 2, 64), k.new_ones(2, 2, 64))
     torch.cuda.synchronize()
     assert torch.equal(before, pool.k)
+
+
+@pytest.mark.parametrize("dtype,cap", [("bf16", 1e4), ("bf16", 1e-6), ("f32", 1e6), ("f32", 1e-6)])
+def test_caps_at_their_limits(dtype, cap):
+    c = U.Case([1, 40, 3], [130, 170, 3], 8, 1, 256, dtype=dtype, page=16, seed=51)
+    pool, batch, q = c.device()
+    U.check_attention(c, paged.attention(pool, batch, q, cap=cap), U.attention_ref(c, cap=cap))

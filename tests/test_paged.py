@@ -219,3 +219,17 @@ def test_plans_without_a_gpu_and_the_bounds_of_one_call():
     for kw in (dict(bf16=True), dict(bf16=False)):
         with pytest.raises(vla.VlaError, match="too many rows"):
             paged.attention_plan(65535, 65535, 1, 64, 4096, 4096, 64, **kw)
+
+
+@pytest.mark.parametrize("dtype,cap,ok", [(1, 1e4, True), (1, 1.1e4, False), (0, 1e8, True), (1, 1e-6, True), (1, 9e-7, False),
+                                          (0, 1e-30, False), (0, -1.0, False), (1, float("nan"), False)])
+def test_caps_that_the_scores_precision_does_not_carry(dtype, cap, ok):
+    pool, batch, att, _ = good()
+    pool.dtype, att.cap = dtype, cap
+    need = ctypes.c_size_t()
+    call = lambda: vla.lib().vla_attention_workspace(ctypes.byref(pool), ctypes.byref(batch), ctypes.byref(att), 0,   # noqa: E731
+                                                     ctypes.byref(need))
+    if ok:
+        assert call() == vla.VLA_OK
+    else:
+        refused(call, "cap")
