@@ -692,15 +692,21 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
       asm volatile("" : "+v"(kt), "+v"(vt));
       // fragments are requested well ahead of their products (LDS answers after
       // a few of these): all keys' first, two groups of the values' before the
-      // softmax (head dim 256 has no registers for that)
+      // softmax. Head dim 256 has registers for two fragments ahead of a product
+      // (one: five capped prompts of 866 tokens 52.8 -> 50.2 us, two of 1500 of 16 heads
+      // 62.4 -> 57.3 on one host; four, or parts of the queries in LDS for them: no faster)
       f32x16 sc[NS];
-      bf16x8 kf[HDP <= 128 ? NS : 1][NC];
       constexpr bool AHEAD = HDP <= 128;
+      bf16x8 kf[AHEAD ? NS : 1][AHEAD ? NC : 2];
       if constexpr (AHEAD) {
 #pragma unroll
         for (int st = 0; st < NS; ++st)
 #pragma unroll
           for (int c = 0; c < NC; ++c) kf[st][c] = read_k(kt, c, st * 32 * Y::ROWB);
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) kf[0][c] = read_k(kt, c, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
       // (at head dim 256 the products go first: five capped prompts of 866 tokens 48.4 -> 47.0 us; at 64 and 128,
@@ -712,8 +718,11 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
         for (int i = 0; i < 16; ++i) sc[st][i] = 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          if constexpr (!AHEAD) kf[0][c] = read_k(kt, c, st * 32 * Y::ROWB);
-          sc[st] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[AHEAD ? st : 0][c], qf[c], sc[st], 0, 0, 0);
+          sc[st] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[AHEAD ? st : 0][AHEAD ? c : c % 2], qf[c], sc[st], 0, 0, 0);
+          if constexpr (!AHEAD) {
+            if (c + 2 < NC) kf[0][c % 2] = read_k(kt, c + 2, 0);
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
       }
       if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(0);
@@ -729,15 +738,28 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, RowsShared<HDP
       }
       softmax_tile<HDP, NS, CAP>(s, sc, sl2, c1, c2, !holes && tile_full(wl, k0, k0 + KT), w.lim, k0, a, it, holes);
       if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(1);
+      if constexpr (AHEAD) {
 #pragma unroll
-      for (int c = 0; c < KT / 16; ++c) {
-        const bf16x8 pf = weights_of(sc[c / 2], c % 2);
-        if constexpr (!AHEAD) values(c);
+        for (int c = 0; c < KT / 16; ++c) {
+          const bf16x8 pf = weights_of(sc[c / 2], c % 2);
 #pragma unroll
-        for (int u2 = 0; u2 < ND; ++u2)
-          s.o[u2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c % 2][u2], pf, s.o[u2], 0, 0, 0);
-        if constexpr (AHEAD)
+          for (int u2 = 0; u2 < ND; ++u2)
+            s.o[u2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c % 2][u2], pf, s.o[u2], 0, 0, 0);
           if (c + 2 < KT / 16) values(c + 2);
+        }
+      } else {
+        constexpr int N = KT / 16 * ND;
+        bf16x8 vr[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) vr[n] = read_vt<HDP>(vt, n % ND, n / ND * 16 * Y::ROWB);
+        const bf16x8 pf[2] = {weights_of(sc[0], 0), weights_of(sc[0], 1)};
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          s.o[n % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vr[n % 2], pf[n / ND], s.o[n % ND], 0, 0, 0);
+          if (n + 2 < N) vr[n % 2] = read_vt<HDP>(vt, (n + 2) % ND, (n + 2) / ND * 16 * Y::ROWB);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
       if constexpr (HDP == 256) __builtin_amdgcn_s_setprio(0);
     }
