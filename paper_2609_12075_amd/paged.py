@@ -6,7 +6,8 @@ which pages it lies. ``append`` writes a step's keys and values (rotating
 queries and keys on the way), ``attention`` attends over the cache and
 ``shared_attention`` reads a context that all requests begin with once for
 the batch. Calls run on the pool's device, on `stream` or that device's
-current stream.
+current stream; tensors that a call allocates belong to that stream (use on
+another one waits for it, and tells the allocator by record_stream).
 """
 from __future__ import annotations
 
