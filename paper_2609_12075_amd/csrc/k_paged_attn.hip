@@ -1432,10 +1432,11 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedAttnArgs a) {
     s *= w0;
 #pragma unroll
     for (int g = 1; g < WPR; ++g) {
-      const float mg = st[tid + g * LPR][0];
-      if (mg == -INFINITY) continue;
-      const float w = __builtin_amdgcn_exp2f(mg - mm);
-      l += st[tid + g * LPR][1] * w;
+      // (as above: a group without keys goes by its sum, as one whose first scores are NaN has no maximum either)
+      const float lg = st[tid + g * LPR][1];
+      if (lg == 0.f) continue;
+      const float w = __builtin_amdgcn_exp2f(st[tid + g * LPR][0] - mm);
+      l += lg * w;
       s += acc[tid + g * LPR] * w;
     }
     m = mm;
