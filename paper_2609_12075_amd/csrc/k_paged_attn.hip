@@ -1323,8 +1323,9 @@ __device__ __forceinline__ void f32_body(const PagedAttnArgs& a, F32Shared<HDP>&
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           const f32x4 x = *reinterpret_cast<const f32x4*>(src + 4 * c);
-          if (w1 != 1.f) o[t][c] = w1 == 0.f ? zero : o[t][c] * w1;
-          if (w2 != 0.f) o[t][c] += x * w2;
+          // (0 times a NaN value that the row sees stays a NaN; a wave without keys has zeros)
+          if (w1 != 1.f) o[t][c] *= w1;
+          o[t][c] += x * w2;
         }
         l[t] = l[t] * w1 + l2 * w2;
         m[t] = mm;

@@ -63,3 +63,24 @@ def test_nan_key_behind_a_common_context(shared, heads, dtype, ranges):
     pool, batch, q = c.device()
     lse = torch.zeros(q.shape[:2], device="cuda")
     check_nan(c, paged.shared_attention(pool, batch, q, shared, lse=lse), lse, 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new,length,heads", [([1], [250], (4, 2, 64)), ([1], [250], (2, 2, 256)),
+                                              ([20, 3], [250, 128], (4, 2, 64)),
+                                              ([300, 222], [320, 400], (32, 8, 128))], ids=str)
+@pytest.mark.parametrize("nan_at,top_at", [(3, 20), (20, 3), (85, 3), (3, 85), (40, 120)])
+def test_nan_value_of_a_weight_that_underflows(nan_at, top_at, new, length, heads, dtype):
+    """A token sees a NaN value with a weight of e^-200, which fp32 holds as 0: 0 times NaN is NaN, in whichever wave
+    of a block the two keys lie (tiles of 16 or 32 keys go to the waves in turn)."""
+    c = U.Case(new, length, *heads, dtype=dtype, page=16, seed=62)
+    c.q.zero_()
+    c.q[..., 0] = 1.0
+    c.k[..., 0] = 0.0
+    page = c.table[0]
+    c.k[page[top_at // 16], 0, top_at % 16, 0] = 200.0
+    c.v[page[nan_at // 16], 0, nan_at % 16, ::5] = math.nan
+    pool, batch, q = c.device()
+    got = paged.attention(pool, batch, q, scale=1.0)
+    U.check_attention(c, got, U.attention_ref(c, scale=1.0))
+    assert torch.isnan(got[c.starts[1] - 1, 0, ::5]).all() and torch.isfinite(got[c.starts[1] - 1, 0, 1::5]).all()
