@@ -437,12 +437,14 @@ __device__ __forceinline__ void softmax_tile(Acc<HDP>& s, f32x16 (&sc)[NS], floa
   for (int i = 1; i < 16 * NS; ++i) mx = vmax(mx, sc[i / 16][i % 16]);
   mx = max_x32(mx);
   if constexpr (!CAP) mx *= sl2;
-  // The reference follows a row's maximum only where that grew by more than
-  // 2^8 (or the row saw its first key): the outputs are rescaled rarely then,
-  // and a weight of up to 2^8 loses nothing in fp32 or, rounded, in bf16. Rows
-  // that have seen nothing keep a reference of 0: no -inf - -inf.
-  if (__ballot(mx > s.m + 8.f)) {
-    const float mn = vmax(s.m, mx), alpha = __builtin_amdgcn_exp2f(s.m - (mn == -INFINITY ? 0.f : mn));
+  // The reference is put 2^8 above a row's maximum and moves only where a score
+  // passes it (or the row saw its first key): the outputs are rescaled rarely
+  // then, no weight is above 1 (values near the type's largest must not
+  // overflow in a sum that is finite), and a row's largest weight, 2^-8 or
+  // more, loses nothing in fp32 or, rounded, in bf16. Rows that have seen
+  // nothing take a reference of 0: no -inf - -inf.
+  if (__ballot(mx > s.m)) {
+    const float mn = vmax(s.m, mx + 8.f), alpha = __builtin_amdgcn_exp2f(s.m - (mn == -INFINITY ? 0.f : mn));
     s.m = mn;
     s.l *= alpha;
 #pragma unroll
@@ -977,9 +979,9 @@ __device__ __forceinline__ void keys_body(const PagedAttnArgs& a, KeysShared<HDP
       mx = vmax(mx, x);
     }
     mx = max_x32(max_x16(mx));
-    // (the reference follows only a growth of 2^8, as in softmax_tile)
-    if (__ballot(mx > m + 8.f)) {
-      const float mn = vmax(m, mx), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.f : mn));
+    // (the reference lies 2^8 above the maximum that it was taken at, as in softmax_tile)
+    if (__ballot(mx > m)) {
+      const float mn = vmax(m, mx + 8.f), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.f : mn));
       const bool some = __ballot(m != -INFINITY) != 0;      // (else there is nothing yet to rescale)
       m = mn;
       l *= alpha;

@@ -38,8 +38,8 @@ struct PagedAttnArgs {
   int causal, window;
   const int32_t* prefix;
   int shared_len;                              // keys below it lie on the pages of request 0
-  // Scratch: unnormalised outputs [n_tok][n_q][slots][hd], then (max in log2
-  // units, sum) pairs [n_tok][n_q][slots], fp32. A sum of -1 in slot 0: the
+  // Scratch: unnormalised outputs [n_tok][n_q][slots][hd], then (reference of
+  // the weights in log2 units, sum) pairs [n_tok][n_q][slots], fp32. A sum of -1 in slot 0: the
   // row's output is written already.
   float* ws;
   // set by the launcher, per launch

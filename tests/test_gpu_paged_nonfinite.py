@@ -84,3 +84,42 @@ def test_nan_value_of_a_weight_that_underflows(nan_at, top_at, new, length, head
     got = paged.attention(pool, batch, q, scale=1.0)
     U.check_attention(c, got, U.attention_ref(c, scale=1.0))
     assert torch.isnan(got[c.starts[1] - 1, 0, ::5]).all() and torch.isfinite(got[c.starts[1] - 1, 0, 1::5]).all()
+
+
+# (new, length, heads, page, common context), the kernels and key tiles a range of the parts, and a key that is
+# neither in the first tile that its wave takes of a range nor in the last request's own part
+LARGE = [
+    (([500, 1, 99], [900, 700, 99], (8, 2, 64), 16, 0), [("keys", 32)], 300),
+    (([1] * 64, [600] * 64, (32, 8, 128), 16, 0), [("keys", 20)], 300),
+    (([1] * 48, [600] * 48, (8, 8, 256), 16, 0), [("keys", 8)], 326),
+    (([900, 77, 523], [1200, 300, 600], (16, 8, 64), 1, 0), [("rows2", 20)], 270),
+    (([300, 30], [2500, 1900], (8, 2, 256), 16, 0), [("rows2", 16)], 1224),
+    (([300, 290, 280, 299, 271, 300], [300, 310, 280, 299, 271, 333], (32, 32, 128), 1, 0), [("rows8", 6)], 200),
+    (([16, 3, 9, 20] * 6, [1054, 1027, 1174, 1044] * 6, (8, 2, 256), 16, 1024), [("rows", 8), ("keys", 12)], 356),
+    (([1] * 64, [2088] * 64, (32, 8, 128), 16, 2048), [("rows", 4), ("keys", 4)], 356),
+    (([1] * 40, [2078] * 40, (8, 8, 128), 16, 2048), [("keys", 8), ("keys", 4)], 396),
+]
+
+
+@pytest.mark.parametrize("shape,parts,at", LARGE, ids=lambda x: str(x)[-60:])
+def test_values_near_the_largest_one(shape, parts, at):
+    """Values of 2^123: a weighted sum of them holds as long as no weight is above 1. The scores are 0 but for one key,
+    of e^5 (2^7.2) times the weight of the keys before it."""
+    new, length, heads, page, shared = shape
+    c = U.Case(new, length, *heads, page=page, seed=63, shared=shared)
+    p = plan_of(c, shared)
+    assert [(x[0], x[2]) for x in p] == parts, p
+    c.q.zero_()
+    c.q[..., 0] = 1.0
+    c.k[..., 0] = 0.0
+    for r, n in enumerate(length):
+        if at < n:
+            c.k[c.table[r][at // page], :, at % page, 0] = 5.0
+    c.v = (c.v.float() * 2.0 ** 123).bfloat16()
+    pool, batch, q = c.device()
+    lse = torch.zeros(q.shape[:2], device="cuda")
+    kw = dict(lse=lse, scale=1.0)
+    got = paged.shared_attention(pool, batch, q, shared, **kw) if shared else paged.attention(pool, batch, q, **kw)
+    ref = U.attention_ref(c, scale=1.0)
+    assert torch.isfinite(got).all()
+    U.check_attention(c, got, ref, lse)
