@@ -132,7 +132,8 @@ typedef struct {
 
 /* Bytes of scratch that vla_paged_attention (shared_len 0) or
  * vla_shared_attention needs with these arguments (q, o, ws and the device
- * buffers of the batch are not looked at). Host only, no GPU needed. */
+ * buffers of the batch are not looked at; of cap and prefix, whether there is
+ * one, which changes how the attention is launched). Host only, no GPU needed. */
 vla_status vla_attention_workspace(const vla_kv_pool* pool, const vla_ragged* batch, const vla_attention_args* args,
                                    int shared_len, size_t* bytes);
 

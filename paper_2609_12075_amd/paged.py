@@ -250,13 +250,24 @@ def shared_attention(pool: KVPool, batch: Batch, q, shared_len: int, out=None, l
     return _attend(pool, batch, q, int(shared_len), out, lse, scale, cap, causal, window, prefix, ws, stream)
 
 
-def workspace_bytes(pool: KVPool, batch: Batch, n_q: int, shared_len: int = 0, causal: bool = True,
-                    window: int = 0) -> int:
-    """vla_attention_workspace: scratch bytes of such an attention (host only)."""
-    a = AttentionArgsC(n_q=n_q, causal=int(bool(causal)), window=window)
-    need = ctypes.c_size_t()
-    vla._check(_lib().vla_attention_workspace(pool.ref, batch.ref, ctypes.byref(a), shared_len, ctypes.byref(need)))
-    return need.value
+def workspace_bytes(pool: KVPool, batch: Batch, n_q: int, shared_len: int = 0, causal: bool = True, window: int = 0,
+                    cap: Optional[float] = None, prefix=None) -> int:
+    """vla_attention_workspace: scratch bytes of such an attention (host only).
+    A capped call may need more than another one, and so may one with a
+    prefix: cap and prefix are those of the call (prefix False: none); with
+    either left out, what is told suffices with and without it."""
+    caps = (0.0, 1.0) if cap is None else (cap,)
+    prefixes = (False, causal) if prefix is None else (prefix is not False,)
+    most = 0
+    for c in caps:
+        for p in prefixes:
+            # (of the prefix only whether there is one is looked at)
+            a = AttentionArgsC(n_q=n_q, causal=int(bool(causal)), window=window, cap=c, prefix=64 if p else None)
+            need = ctypes.c_size_t()
+            vla._check((_L or _lib()).vla_attention_workspace(pool.ref, batch.ref, ctypes.byref(a), shared_len,
+                                                              ctypes.byref(need)))
+            most = max(most, need.value)
+    return most
 
 
 def attention_plan(n_req: int, n_tok: int, max_new: int, max_len: int, n_q: int, n_kv: int, head_dim: int, page: int = 16,
