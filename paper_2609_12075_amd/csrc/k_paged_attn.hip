@@ -1592,6 +1592,14 @@ size_t paged_attention_ws(const PagedAttnArgs& a, const PagedPlan& p) {
   return p.slots > 1 ? (size_t)a.bt.n_tok * a.n_q * p.slots * (a.kv.hd + 2) * 4 : 0;
 }
 
+// The kernels that the launches below know, of a part of n: another one in the
+// plan is an error, not a launch that reads bf16 as fp32.
+static bool has_kernel(int et, int k, int hdp, int part, int n) {
+  if (et == ET_F32) return k == PAGED_F32 || (k == PAGED_F32R && n == 1 && hdp < 256);
+  if (n == 2) return k == PAGED_KEYS || (k == PAGED_ROWS && part == 0);
+  return k == PAGED_KEYS || k == PAGED_ROWS2 || (k == PAGED_ROWS8 && hdp == 128);
+}
+
 template <int HDP, bool CAP>
 static void launch_one(const PagedAttnArgs& a, int kernel, hipStream_t s) {
   const dim3 grid((unsigned)a.tiles * a.kv.n_kv, a.ranges);
@@ -1638,6 +1646,8 @@ void launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& p, int et, 
   int slot = 0;
   for (int i = 0; i < p.n_parts; ++i) {
     const PagedPart& q = p.part[i];
+    VLA_REQUIRE(has_kernel(et, q.kernel, p.hdp, i, p.n_parts),
+                "no paged attention kernel " + std::to_string(q.kernel) + " for head dim " + std::to_string(p.hdp));
     PagedAttnArgs& b = part[i];
     const bool flat = p.n_parts == 2 && i == 0;
     b.klo = p.n_parts == 2 && i == 1 ? a.shared_len : 0;
