@@ -66,8 +66,12 @@ void fill(const vla_kv_pool* p, const vla_ragged* b, bool buffers, PagedKV& kv, 
     VLA_REQUIRE(p->k && p->v && aligned(p->k, 16) && aligned(p->v, 16), "pool k and v must be 16-byte aligned buffers");
     VLA_REQUIRE(b->start && b->kv_len && (b->pages || b->pages_stride == 0), "null start, kv_len or pages");
     VLA_REQUIRE(aligned(b->start, 4) && aligned(b->kv_len, 4) && aligned(b->pages, 4), "start, kv_len and pages must be 4-byte aligned");
-    static int ndev = 0;                       // (does not change while the process runs)
-    if (ndev == 0) VLA_HIP(hipGetDeviceCount(&ndev));
+    // (does not change while the process runs; first calls of several threads wait for one of them)
+    static const int ndev = [] {
+      int n = 0;
+      VLA_HIP(hipGetDeviceCount(&n));
+      return n;
+    }();
     VLA_REQUIRE(p->device >= 0 && p->device < ndev, "device " + std::to_string(p->device) + " not present");
   }
   kv.k = p->k; kv.v = p->v;

@@ -39,3 +39,30 @@ def test_every_plan_names_a_kernel_of_its_type(bf16):
             kt = 16 if name.startswith("f32") else 16 * wide if name == "keys" else 32 * wide
             assert chunk * ranges * kt >= keys, (p, kw)
     assert seen == ({"keys", "rows", "rows2", "rows8"} if bf16 else {"f32", "f32_rows"})
+
+
+def test_first_calls_of_several_threads_answer_alike():
+    """Each thread's first call counts the devices: the same answer for all of them (an error: device 99 is not
+    there, or there is no GPU)."""
+    import subprocess
+    import sys
+    code = """
+import ctypes, threading
+from paper_2609_12075_amd import paged
+L = paged._lib()
+pool = paged.KVPoolC(99, 1, 2, 64, 16, 8, 4096, 8192, 2048, 1024, 64)
+batch = paged.RaggedC(3, 6, 4, 64, 16, 32, 64, 4)
+att = paged.AttentionArgsC(q=256, o=512, q_tok_stride=256, q_head_stride=64, o_tok_stride=256, o_head_stride=64, n_q=4, causal=1)
+go, got = threading.Barrier(16), []
+def call():
+    go.wait()
+    for _ in range(20):
+        got.append((L.vla_paged_attention(ctypes.byref(pool), ctypes.byref(batch), ctypes.byref(att), None), L.vla_last_error()))
+ts = [threading.Thread(target=call) for _ in range(16)]
+[t.start() for t in ts]
+[t.join() for t in ts]
+assert len(got) == 320 and len(set(got)) == 1 and got[0][0] != 0 and got[0][1], set(got)
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300,
+                       cwd=__file__.rsplit("/", 2)[0])
+    assert r.returncode == 0, r.stderr[-2000:]
