@@ -190,6 +190,8 @@ def append(pool: KVPool, batch: Batch, k, v, q=None, q_out=None, positions=None,
         if q_out is None:
             q_out = _empty(q.shape, q.dtype, pool, stream)
         qo = _rows(q_out, "q_out", pool, batch, n_q)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
     kp, kt, kh = _rows(k, "k", pool, batch, pool.n_kv)
     vp, vt, vh = _rows(v, "v", pool, batch, pool.n_kv)
     pos = None if positions is None else _i32(positions, "positions", (batch.n_tok, n), pool.device)
