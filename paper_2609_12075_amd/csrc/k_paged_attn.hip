@@ -301,8 +301,11 @@ __device__ __forceinline__ bf16x8 read_k(unsigned at, int c, int off) {
 // of this KV head's rows; -1: not there), entries w0 .. w0 + PW - 1.
 constexpr int PW = 256;
 
-// Fills the window of page offsets from entry e0 on; true where a page that
-// the item's keys need is not there.
+// Fills the window of page offsets from entry e0 on; true where one of its pages
+// below the item's last key is not there, whether some row sees its keys or not
+// (the block then looks the pages of its keys up one by one, in all tiles from
+// there on: 8000 keys behind a window of 1024, one token of 32 heads of 128,
+// 13.4 us with the pages before the window given back, 11.7 with all there).
 // (all threads of the block, at least PW, call it, and none reads the window or the flags
 // of an earlier call any more; ends with a barrier; `guessed`: this
 // thread's entry of the window from entry `guess` on, requested earlier)
@@ -598,7 +601,7 @@ __device__ __forceinline__ void put_stats(const PagedAttnArgs& a, const Item& it
 // (64 keys a tile; 32 at head dim 256.) Eight waves of rows and two tiles a
 // round where there are rows enough: half the loads and round overhead of four.
 // Two groups of four where the blocks are few: their results meet in LDS.
-// A prompt of 8191 of 32 heads of 128, causal: 529-545 us, 1.03 PFLOP/s at the
+// A prompt of 8191 of 32 heads of 128, causal: 529-569 us, 1.03 PFLOP/s at the
 // 1.9 GHz to which the chip throttles (a product of 8192^3 reaches 1.42): the
 // matrix pipe is busy for 46 % of the time, the vector pipe for 44 % (a wave's
 // softmax of a tile takes as long as its products). Measured slower: the scores of
@@ -1474,7 +1477,8 @@ static int round_tiles(int k) { return k == PAGED_KEYS ? 4 : k == PAGED_ROWS2 ||
 // a block's bytes at what one CU takes in, or all bytes at the memory's rate
 // (requests' keys differ) or the L2's; a part of a last block's rounds, as
 // lengths differ and it runs alone; and, where a row has several ranges, the merge's
-// launch and their outputs. Starts and rounds are measured; the model
+// launch and their outputs. Ranges are counted over all keys up to max_len, those
+// before a window too, which no tile's list holds (a prefix may lie there). Starts and rounds are measured; the model
 // need only be right where the kernels' times differ much. (One request's token
 // over 881 keys of 8 heads of 256: ranges of 64 keys 10.5 us, 128 11.9, 256
 // 13.8. 64 tokens over up to 8101 keys of 8 heads of 128: one range 272 us, four

@@ -97,7 +97,7 @@ __device__ __forceinline__ ReqSpan span_of(const RaggedBatch& b, int r, int page
 
 // The request of a token: the last r with start[r] <= tok (requests without
 // tokens share their start with the next one); n_req when tok lies behind the
-// last. A wavefront looks at 64 starts at a time, so up to 4096 requests take
+// last. A wavefront looks at 64 starts at a time, so up to 4095 requests take
 // two rounds of loads. Wave-uniform tok; all lanes of the wave call it.
 __device__ __forceinline__ int request_of(const RaggedBatch& b, int tok) {
   const int lane = threadIdx.x & 63;
