@@ -25,7 +25,7 @@
  * probabilities are rounded to bf16 before they weigh bf16 values (relative to
  * the row's largest, so an output is off by at most 2^-8 of its row's largest
  * value). Weights are at most 1 until the sum over the values is divided by
- * theirs: values whose sum so weighted stays below 2^128 do not overflow.
+ * theirs: values below 2^128 / (keys that the token sees) do not overflow.
  * Rotation angles are reduced in fp64, rotation is fp32. VLA_F32 calls
  * compute in fp32 throughout.
  */

@@ -442,8 +442,8 @@ __device__ __forceinline__ void softmax_tile(Acc<HDP>& s, f32x16 (&sc)[NS], floa
   if constexpr (!CAP) mx *= sl2;
   // The reference is put 2^8 above a row's maximum and moves only where a score
   // passes it (or the row saw its first key): the outputs are rescaled rarely
-  // then, no weight is above 1 (values near the type's largest must not
-  // overflow in a sum that is finite), and a row's largest weight, 2^-8 or
+  // then, no weight is above 1 (weights of 2^8 would let values overflow that
+  // a sum of weights of at most 1 holds), and a row's largest weight, 2^-8 or
   // more, loses nothing in fp32 or, rounded, in bf16. Rows that have seen
   // nothing take a reference of 0: no -inf - -inf.
   if (__ballot(mx > s.m)) {
